@@ -262,6 +262,159 @@ mod_status mod_block_sparse_attn_fwd_noalloc(const mod_shape* shape, const void*
                                              const int32_t* kv_cnt, float scale, void* o, float* lse,
                                              void* stream);
 
+/* ---- the cached layer ------------------------------------------------------
+ *
+ * A video that is made in chunks of frames keeps the keys and values of the
+ * frames made so far.  Per layer and chunk: rotate the new queries and keys
+ * (mod_rope_fwd), write the new keys and values into the cache
+ * (mod_cache_write) and attend from the new queries to what the cache holds
+ * (mod_cache_attn_fwd), over every block or over lists of kept blocks such as
+ * mod_predict_block_mask selects.  Single tokens are served by the same calls.
+ *
+ * The operands may sit as the projection left them: a tensor argument with a
+ * mod_strides is [B, H, L, d] with d contiguous and the other axes that many
+ * elements apart (NULL: contiguous), the pointer 16-byte aligned and the
+ * strides multiples of 8.
+ *
+ * A token's position is first + starts[b] + l for token l of sequence b:
+ * `first` comes from the host, `starts` ([B] int32, device) or NULL for zeros,
+ * so a captured call can advance.  Entries of `starts`, `counts` and `kv_len`
+ * are read on the device; out of range ones are handled as stated, not
+ * reported. */
+typedef struct {
+    int64_t b, h, l;   /* elements between sequences, heads, tokens */
+} mod_strides;
+
+/* Rotary positions over the axes time, height and width of a video (an image:
+ * frames = 1).  The first dims[0] channels of a head are rotated by the
+ * token's frame, the next dims[1] by its row, the next dims[2] by its column;
+ * channels past their sum are copied.  Pair j of an axis of w channels turns by
+ * position * theta^(-2j/w):
+ *   y0 = x0 cos - x1 sin,   y1 = x0 sin + x1 cos.
+ * Position p is frame p / (height*width), row p / width mod height, column
+ * p mod width (frame-first tokens, as everywhere here). */
+typedef enum {
+    MOD_ROPE_ADJACENT = 0,   /* pair j: channels 2j, 2j+1 of the axis       */
+    MOD_ROPE_HALVES = 1      /* pair j: channels j, j + w/2 of the axis     */
+} mod_rope_pairing;
+
+typedef struct {
+    int d;                      /* head dimension: 64 or 128                          */
+    int dims[3];                /* channels per axis, even, >= 0, sum in [2, d]       */
+    int frames, height, width;  /* positions of each axis; frames*height*width < 2^31 */
+    double theta;               /* > 1                                                */
+    int pairing;                /* mod_rope_pairing                                   */
+} mod_rope_params;
+
+typedef struct mod_rope mod_rope;   /* opaque, library-owned */
+
+/* Build the (cos, sin) tables of the axes on the host in fp64 and upload them
+ * as fp32 (4 * (frames*dims[0] + height*dims[1] + width*dims[2]) bytes on the
+ * current device).  Synchronous.  The handle is not changed by its use: any
+ * number of calls and streams of that device may share it. */
+mod_status mod_rope_create(const mod_rope_params* params, mod_rope** out);
+
+/* Release the handle (waits for the device).  NULL is accepted. */
+mod_status mod_rope_destroy(mod_rope* rope);
+
+/* y = R x in fp32, rounded to bf16 once.  B, H, L, d, text_tokens of the shape
+ * are used (block is not, frame_tokens must be 0 or height*width): the last
+ * text_tokens tokens have no position and are copied.  The rotated channels of
+ * a token whose position is outside [0, frames*height*width) become NaN (with
+ * starts NULL: MOD_ERR_INVALID_ARG).  y may be x where the strides are equal; they must not
+ * overlap otherwise. */
+mod_status mod_rope_fwd(const mod_rope* rope, const mod_shape* shape, const void* x, const mod_strides* x_strides,
+                        void* y, const mod_strides* y_strides, int first, const int32_t* starts, void* stream);
+
+/* The gradient of mod_rope_fwd with respect to x: dx = R^T dy. */
+mod_status mod_rope_bwd(const mod_rope* rope, const mod_shape* shape, const void* dy, const mod_strides* dy_strides,
+                        void* dx, const mod_strides* dx_strides, int first, const int32_t* starts, void* stream);
+
+/* A cache of keys and values in 8 bits with one fp32 scale per block of
+ * `block` tokens and head; a code c stands for c * scale. */
+typedef enum {
+    MOD_CACHE_E4M3 = 0,   /* 4 exponent and 3 fraction bits, largest 448       */
+    MOD_CACHE_INT8 = 1    /* integers -127 .. 127                              */
+} mod_cache_format;
+
+typedef struct {
+    int B;          /* sequences                            */
+    int H;          /* key/value heads                      */
+    int capacity;   /* tokens a sequence can hold, <= 2^24  */
+    int d;          /* 64 or 128                            */
+    int block;      /* tokens that share a scale: 64 or 128 */
+    int format;     /* mod_cache_format                     */
+} mod_cache_shape;
+
+/* Device memory of the caller: codes [B, H, capacity, d], one byte each,
+ * 16-byte aligned, and scales [B, H, mod_cache_blocks(shape)].  Needs no
+ * initial values. */
+typedef struct {
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+} mod_cache;
+
+/* ceil(capacity / block); 0 for a null or invalid shape. */
+int mod_cache_blocks(const mod_cache_shape* shape);
+
+/* Write L tokens of k and v (bf16) at positions first + starts[b] + l,
+ * quantised.  Only the first counts[b] tokens of sequence b are written (NULL:
+ * all L; values are clamped to [0, L]), and none of a sequence whose start is
+ * outside [0, capacity); tokens past the capacity are dropped (with starts
+ * NULL, first + L <= capacity or MOD_ERR_INVALID_ARG).
+ * A block's scale is s = S(amax), amax the largest magnitude written into the
+ * block by this call:
+ *   E4M3   the smallest power of two with amax / s <= 448 (a floating code
+ *          gains nothing from a finer scale, and x / s is exact)
+ *   INT8   amax / 127 rounded to fp32
+ * at least 2^-126, and 0 for amax = 0.  A write that starts inside a block
+ * continues it: the scale becomes max(old scale, S(amax)), and where it grew
+ * the codes of the block's earlier tokens are rounded again under it (for
+ * E4M3 exact but for magnitudes under 2^-6 of the scale).  The new codes are
+ * x / s rounded to the nearest, ties to even, decided without error.
+ * What a sequence held past the end of the write is dropped: those codes stay
+ * in memory but stand for nothing.  A block that receives an infinity or NaN
+ * gets the scale NaN (codes of this call 0), so that what is read from it is
+ * NaN until a write starts it anew. */
+mod_status mod_cache_write(const mod_cache_shape* shape, const mod_cache* cache, const void* k,
+                           const mod_strides* k_strides, const void* v, const mod_strides* v_strides, int L,
+                           int first, const int32_t* starts, const int32_t* counts, void* stream);
+
+/* What the tokens at those positions stand for, code * scale rounded to bf16
+ * once.  Rows of tokens that mod_cache_write would not write are left as they
+ * were.  k or v may be NULL (not read). */
+mod_status mod_cache_read(const mod_cache_shape* shape, const mod_cache* cache, void* k, const mod_strides* k_strides,
+                          void* v, const mod_strides* v_strides, int L, int first, const int32_t* starts,
+                          const int32_t* counts, void* stream);
+
+/* Workspace of mod_cache_attn_fwd in bytes, for at most max_len cached tokens
+ * (0: none needed, or an invalid argument).  Owned by the caller; two calls in
+ * flight at once (two streams, or two captured graphs) need two. */
+size_t mod_cache_attn_workspace_bytes(const mod_cache_shape* shape, int Hq, int Lq, int max_len);
+
+/* Attention of Lq new queries over the cache: for query token p of head h,
+ *   O_p = sum over kept cached tokens t of softmax_t(scale * Q_p . K_t) V_t,
+ * K_t and V_t what the codes of head h / (Hq / H) stand for, and lse_p as in
+ * mod_block_sparse_attn_fwd.  Hq must be a multiple of H.
+ * q, o: bf16 [B, Hq, Lq, d]; lse: fp32 [B, Hq, Lq] or NULL.  Sequence b holds
+ * kv_len[b] tokens ([B] int32, device, clamped to [0, max_len]; NULL: max_len);
+ * 0 <= max_len <= capacity.
+ * kv_idx, kv_cnt: both NULL (every block), or lists over the n = ceil(max_len
+ * / block) blocks for every block of `block` query tokens (nq = ceil(Lq /
+ * block)): kv_idx [B, Hq, nq, n], kv_cnt [B, Hq, nq] (clamped to [0, n]), the
+ * layout of mod_predict_block_mask; entries outside [0, n) and blocks past the
+ * sequence's end are skipped, each block is listed at most once.
+ * A row that keeps no token gives O = 0 and lse = -inf.  scale = 0 means
+ * 1/sqrt(d).  q, k and v enter bf16 MFMA products without error (every code is
+ * a bf16 number); probabilities, times the value scale, are rounded to bf16;
+ * sums, softmax and accumulation are fp32.  The result does not depend on
+ * anything outside the sequence's own tokens, and is the same in every run. */
+mod_status mod_cache_attn_fwd(const mod_cache_shape* shape, const mod_cache* cache, const void* q, int Hq, int Lq,
+                              int max_len, const int32_t* kv_len, const int32_t* kv_idx, const int32_t* kv_cnt,
+                              float scale, void* o, float* lse, void* workspace, size_t ws_bytes, void* stream);
+
 /* ---- introspection (synchronous copies to host memory; for tests) ---- */
 
 /* The sizes below count the nv video blocks (nv = n without text tokens). */

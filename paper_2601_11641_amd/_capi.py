@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, c_double, c_float, c_int, c_int32, c_size_t, c_void_p
+from ctypes import POINTER, c_double, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 import numpy as np
 
@@ -26,6 +26,10 @@ MOD_ERR_NOMEM = 5
 MOD_BUDGET_TOPK = 0
 MOD_BUDGET_MASS = 1
 MOD_BUDGET_PATTERN = 2
+MOD_ROPE_ADJACENT = 0
+MOD_ROPE_HALVES = 1
+MOD_CACHE_E4M3 = 0
+MOD_CACHE_INT8 = 1
 
 
 class ModError(RuntimeError):
@@ -46,6 +50,24 @@ class mod_params(ctypes.Structure):
 
 class mod_budget(ctypes.Structure):
     _fields_ = [("mode", c_int), ("density", c_float), ("mass", c_float), ("patterns", c_int)]
+
+
+class mod_strides(ctypes.Structure):
+    _fields_ = [("b", c_int64), ("h", c_int64), ("l", c_int64)]
+
+
+class mod_rope_params(ctypes.Structure):
+    _fields_ = [("d", c_int), ("dims", c_int * 3), ("frames", c_int), ("height", c_int), ("width", c_int),
+                ("theta", c_double), ("pairing", c_int)]
+
+
+class mod_cache_shape(ctypes.Structure):
+    _fields_ = [("B", c_int), ("H", c_int), ("capacity", c_int), ("d", c_int), ("block", c_int),
+                ("format", c_int)]
+
+
+class mod_cache(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p)]
 
 
 # torch bundles its own HIP runtime (SONAME libamdhip64.so.7).  Loading torch
@@ -79,6 +101,21 @@ _SIGS = {
     "mod_block_sparse_attn_fwd_noalloc": (c_int, [POINTER(mod_shape), c_void_p, c_void_p, c_void_p,
                                                   c_void_p, c_void_p, c_float, c_void_p, c_void_p,
                                                   c_void_p]),
+    "mod_rope_create": (c_int, [POINTER(mod_rope_params), POINTER(c_void_p)]),
+    "mod_rope_destroy": (c_int, [c_void_p]),
+    "mod_rope_fwd": (c_int, [c_void_p, POINTER(mod_shape), c_void_p, POINTER(mod_strides), c_void_p,
+                             POINTER(mod_strides), c_int, c_void_p, c_void_p]),
+    "mod_rope_bwd": (c_int, [c_void_p, POINTER(mod_shape), c_void_p, POINTER(mod_strides), c_void_p,
+                             POINTER(mod_strides), c_int, c_void_p, c_void_p]),
+    "mod_cache_blocks": (c_int, [POINTER(mod_cache_shape)]),
+    "mod_cache_write": (c_int, [POINTER(mod_cache_shape), POINTER(mod_cache), c_void_p, POINTER(mod_strides),
+                                c_void_p, POINTER(mod_strides), c_int, c_int, c_void_p, c_void_p, c_void_p]),
+    "mod_cache_read": (c_int, [POINTER(mod_cache_shape), POINTER(mod_cache), c_void_p, POINTER(mod_strides),
+                               c_void_p, POINTER(mod_strides), c_int, c_int, c_void_p, c_void_p, c_void_p]),
+    "mod_cache_attn_workspace_bytes": (c_size_t, [POINTER(mod_cache_shape), c_int, c_int, c_int]),
+    "mod_cache_attn_fwd": (c_int, [POINTER(mod_cache_shape), POINTER(mod_cache), c_void_p, c_int, c_int, c_int,
+                                   c_void_p, c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_void_p, c_size_t,
+                                   c_void_p]),
     "mod_stats_get_anchor": (c_int, [c_void_p, c_int, POINTER(c_double), POINTER(c_int)]),
     "mod_stats_get_pooled": (c_int, [c_void_p, POINTER(c_double), POINTER(c_double)]),
     "mod_stats_get_block_mass": (c_int, [c_void_p, POINTER(c_double)]),
@@ -233,6 +270,160 @@ def mod_block_sparse_attn_fwd_noalloc(shape: mod_shape, q, k, v, kv_idx, kv_cnt,
         _ptr(lse, "lse", "torch.float32"), _stream(stream)), "mod_block_sparse_attn_fwd_noalloc")
 
 
+# ---------------------------------------------------------------- the cached layer
+
+def _here(x, what: str):
+    """The library launches on the current device: a tensor of another one is refused."""
+    if hasattr(x, "data_ptr") and x.is_cuda and x.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} is on {x.device}, but the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _ints(x, B: int, what: str):
+    """[B] int32 on the device, or None."""
+    _here(x, what)
+    if hasattr(x, "shape") and tuple(x.shape) != (B,):
+        raise ValueError(f"{what} must have shape ({B},), got {tuple(x.shape)}")
+    return _ptr(x, what, "torch.int32")
+
+
+def _strided(x, dims, what: str):
+    """Pointer and strides of a [B, H, L, d] bf16 tensor whose channels are
+    contiguous (an int: the address of a contiguous one)."""
+    if x is None or isinstance(x, int):
+        return x, None
+    if not hasattr(x, "data_ptr"):
+        raise TypeError(f"{what}: unsupported argument type {type(x)}")
+    if tuple(x.shape) != tuple(dims):
+        raise ValueError(f"{what} must have shape {tuple(dims)}, got {tuple(x.shape)}")
+    if str(x.dtype) != "torch.bfloat16":
+        raise ValueError(f"{what} must be torch.bfloat16, got {x.dtype}")
+    if not x.is_cuda:
+        raise ValueError(f"{what} must be a device tensor")
+    if x.stride(3) != 1:
+        raise ValueError(f"{what} must have contiguous channels")
+    _here(x, what)
+    # the stride of an axis of one entry is of no account
+    st = [x.stride(i) if x.shape[i] > 1 else 0 for i in range(3)]
+    return x.data_ptr(), ctypes.byref(mod_strides(*st))
+
+
+def make_rope_params(d, dims, grid, theta=10000.0, pairing="adjacent") -> mod_rope_params:
+    """dims: channels per axis, grid: positions per axis (time, height, width)."""
+    m = {"adjacent": MOD_ROPE_ADJACENT, "halves": MOD_ROPE_HALVES}.get(pairing, pairing)
+    return mod_rope_params(d, (c_int * 3)(*dims), *grid, theta, int(m))
+
+
+def make_cache_shape(B, H, capacity, d, block, format="e4m3") -> mod_cache_shape:
+    f = {"e4m3": MOD_CACHE_E4M3, "int8": MOD_CACHE_INT8}.get(format, format)
+    return mod_cache_shape(B, H, capacity, d, block, int(f))
+
+
+def make_cache(k, v, k_scale, v_scale) -> mod_cache:
+    """The cache in these tensors (codes of one byte, fp32 scales), which the
+    caller keeps alive: the struct holds their addresses."""
+    for x, what in ((k, "k"), (v, "v")):
+        if hasattr(x, "element_size") and x.element_size() != 1:
+            raise ValueError(f"{what} must have one byte per code, got {x.dtype}")
+    for x, what in ((k, "k"), (v, "v"), (k_scale, "k_scale"), (v_scale, "v_scale")):
+        _here(x, what)
+    return mod_cache(_ptr(k, "k"), _ptr(v, "v"), _ptr(k_scale, "k_scale", "torch.float32"),
+                     _ptr(v_scale, "v_scale", "torch.float32"))
+
+
+def mod_rope_create(params: mod_rope_params) -> int:
+    h = c_void_p()
+    _check(_lib.mod_rope_create(_ref(params), ctypes.byref(h)), "mod_rope_create")
+    return h.value
+
+
+def mod_rope_destroy(rope) -> None:
+    _check(_lib.mod_rope_destroy(rope), "mod_rope_destroy")
+
+
+def _rope_call(name, rope, shape, x, y, first, starts, stream):
+    dims = (shape.B, shape.H, shape.L, shape.d)
+    src, dst = ("x", "y") if name == "mod_rope_fwd" else ("dy", "dx")
+    xp, xs = _strided(x, dims, src)
+    yp, ys = _strided(y, dims, dst)
+    _check(getattr(_lib, name)(rope, ctypes.byref(shape), xp, xs, yp, ys, first, _ints(starts, shape.B, "starts"),
+                               _stream(stream)), name)
+
+
+def mod_rope_fwd(rope, shape: mod_shape, x, y, first: int = 0, starts=None, stream=None) -> None:
+    """y = R x.  x and y: [B, H, L, d] tensors with any strides over the first
+    three axes (a transposed view of a projection's output, say)."""
+    _rope_call("mod_rope_fwd", rope, shape, x, y, first, starts, stream)
+
+
+def mod_rope_bwd(rope, shape: mod_shape, dy, dx, first: int = 0, starts=None, stream=None) -> None:
+    """dx = R^T dy, the gradient of mod_rope_fwd."""
+    _rope_call("mod_rope_bwd", rope, shape, dy, dx, first, starts, stream)
+
+
+def mod_cache_blocks(shape: mod_cache_shape) -> int:
+    return _lib.mod_cache_blocks(_ref(shape))
+
+
+def _store_call(name, shape, cache, k, v, first, starts, counts, L, stream):
+    if L is None:
+        L = (k if k is not None else v).shape[2]
+    dims = (shape.B, shape.H, L, shape.d)
+    kp, ks = _strided(k, dims, "k")
+    vp, vs = _strided(v, dims, "v")
+    _check(getattr(_lib, name)(ctypes.byref(shape), ctypes.byref(cache), kp, ks, vp, vs, L, first,
+                               _ints(starts, shape.B, "starts"), _ints(counts, shape.B, "counts"),
+                               _stream(stream)), name)
+
+
+def mod_cache_write(shape: mod_cache_shape, cache: mod_cache, k, v, first: int = 0, starts=None, counts=None, L=None,
+                    stream=None) -> None:
+    """Quantise k and v ([B, H, L, d] bf16, any strides over the first three
+    axes; L is needed only with addresses) into the cache."""
+    _store_call("mod_cache_write", shape, cache, k, v, first, starts, counts, L, stream)
+
+
+def mod_cache_read(shape: mod_cache_shape, cache: mod_cache, k, v, first: int = 0, starts=None, counts=None, L=None,
+                   stream=None) -> None:
+    """What the cache holds at those positions into k and v (either may be None)."""
+    _store_call("mod_cache_read", shape, cache, k, v, first, starts, counts, L, stream)
+
+
+def mod_cache_attn_workspace_bytes(shape: mod_cache_shape, Hq: int, Lq: int, max_len: int) -> int:
+    return int(_lib.mod_cache_attn_workspace_bytes(_ref(shape), Hq, Lq, max_len))
+
+
+def mod_cache_attn_fwd(shape: mod_cache_shape, cache: mod_cache, q, max_len: int, kv_len, kv_idx, kv_cnt,
+                       scale: float, o, lse=None, workspace=None, ws_bytes: int = 0, stream=None, Hq=None,
+                       Lq=None) -> None:
+    """q, o: contiguous [B, Hq, Lq, d] (with addresses, pass Hq and Lq).
+    workspace=None: a device buffer is allocated for the call (pass one to
+    keep allocations out of a loop)."""
+    if hasattr(q, "shape"):
+        if q.dim() != 4 or q.shape[0] != shape.B or q.shape[3] != shape.d:
+            raise ValueError(f"q must have shape ({shape.B}, Hq, Lq, {shape.d}), got {tuple(q.shape)}")
+        Hq, Lq = q.shape[1], q.shape[2]
+    n, nq = -(-max_len // shape.block), -(-Lq // shape.block)
+    for x, what, dims in ((o, "o", (shape.B, Hq, Lq, shape.d)), (lse, "lse", (shape.B, Hq, Lq)),
+                          (kv_idx, "kv_idx", (shape.B, Hq, nq, n)), (kv_cnt, "kv_cnt", (shape.B, Hq, nq))):
+        if hasattr(x, "shape") and tuple(x.shape) != dims:
+            raise ValueError(f"{what} must have shape {dims}, got {tuple(x.shape)}")
+    for x, what in ((q, "q"), (o, "o"), (lse, "lse"), (kv_idx, "kv_idx"), (kv_cnt, "kv_cnt"),
+                    (workspace, "workspace")):
+        _here(x, what)
+    st = _stream(stream)
+    if workspace is None and hasattr(q, "device"):
+        ws_bytes = mod_cache_attn_workspace_bytes(shape, Hq, Lq, max_len)
+        if ws_bytes > 0:
+            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+            if st != torch.cuda.current_stream().cuda_stream:   # its memory waits for that stream's use of it
+                workspace.record_stream(torch.cuda.ExternalStream(st))
+    _check(_lib.mod_cache_attn_fwd(
+        ctypes.byref(shape), ctypes.byref(cache), _ptr(q, "q", "torch.bfloat16"), Hq, Lq, max_len,
+        _ints(kv_len, shape.B, "kv_len"), _ptr(kv_idx, "kv_idx", "torch.int32"),
+        _ptr(kv_cnt, "kv_cnt", "torch.int32"), float(scale), _ptr(o, "o", "torch.bfloat16"),
+        _ptr(lse, "lse", "torch.float32"), _ptr(workspace, "workspace"), ws_bytes, st), "mod_cache_attn_fwd")
+
+
 def _dbl(n):
     a = np.empty(n, dtype=np.float64)
     return a, a.ctypes.data_as(POINTER(c_double))
@@ -310,3 +501,46 @@ class Stats:
 
     def __exit__(self, *exc):
         self.close()
+
+
+class Rope:
+    """Owner of a mod_rope handle (destroyed on close / garbage collection)."""
+
+    def __init__(self, params: mod_rope_params):
+        self.handle = None
+        self.params = params
+        self.handle = mod_rope_create(params)
+
+    def close(self):
+        if self.handle:
+            mod_rope_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+
+class Cache:
+    """The tensors of a cache and its descriptors: k, v [B, H, capacity, d]
+    uint8, k_scale, v_scale [B, H, n] fp32, `ref` for the calls."""
+
+    def __init__(self, shape: mod_cache_shape, device="cuda"):
+        n = mod_cache_blocks(shape)
+        if n == 0:
+            raise ModError(MOD_ERR_INVALID_ARG, "mod_cache_blocks", mod_last_error())
+        self.shape, self.n = shape, n
+        codes = (shape.B, shape.H, shape.capacity, shape.d)
+        self.k = torch.empty(codes, dtype=torch.uint8, device=device)
+        self.v = torch.empty(codes, dtype=torch.uint8, device=device)
+        self.k_scale = torch.empty((shape.B, shape.H, n), dtype=torch.float32, device=device)
+        self.v_scale = torch.empty((shape.B, shape.H, n), dtype=torch.float32, device=device)
+        self.ref = make_cache(self.k, self.v, self.k_scale, self.v_scale)

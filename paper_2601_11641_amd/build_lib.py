@@ -18,7 +18,7 @@ LIB = os.path.join(HERE, "libmoddit.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
-SOURCES = ["predictor.hip", "attn_fwd.hip", "capi.cpp"]
+SOURCES = ["predictor.hip", "attn_fwd.hip", "rope.hip", "cache.hip", "cache_attn.hip", "capi.cpp", "capi_cache.cpp"]
 
 # Packed fp32 VALU forms are kept out of the generated code on purpose.
 # MFMA results are kept in architectural VGPRs (VGPR form) so that the

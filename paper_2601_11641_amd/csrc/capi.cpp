@@ -14,8 +14,10 @@
 #include <vector>
 
 namespace {
-
 thread_local std::string g_last_error;
+}
+
+namespace moddit {
 
 mod_status fail(mod_status st, const char* fmt, ...) {
     char buf[512];
@@ -30,6 +32,13 @@ mod_status fail(mod_status st, const char* fmt, ...) {
 mod_status hip_fail(hipError_t e, const char* what) {
     return fail(MOD_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace moddit
+
+namespace {
+
+using moddit::fail;
+using moddit::hip_fail;
 
 int ceil_div(int a, int b) { return (a + b - 1) / b; }
 

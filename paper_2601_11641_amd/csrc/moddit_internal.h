@@ -5,10 +5,16 @@
 
 #include <hip/hip_runtime.h>
 
+#include "../../include/moddit.h"
+
 #include <cstddef>
 #include <cstdint>
 
 namespace moddit {
+
+// Set mod_last_error()'s message (printf form) and return `st`.
+mod_status fail(mod_status st, const char* fmt, ...);
+mod_status hip_fail(hipError_t e, const char* what);
 
 constexpr int kMaxBlocks = 4096;     // largest n (selection keeps a row in LDS)
 constexpr int kSolveSplit = 16;     // k-chunks of the Schur-complement product (fixed: deterministic sum)
@@ -81,5 +87,42 @@ hipError_t noalloc_scratch(void** out);
 hipError_t launch_stat_count(const uint16_t* q, const uint16_t* k, const int32_t* kv_idx,
                              const int32_t* kv_cnt, const float* lse, float scale, float log_eta,
                              double* stat, int BH, int L, int d, int bs, int n, int nv, hipStream_t s);
+
+// ---- the cached layer: rotary positions, 8-bit cache, attention over it ----
+
+// A [B, H, L, d] tensor of bf16 with d contiguous; strides in elements.
+struct Strided {
+    uint16_t* p;
+    long b, h, l;
+};
+
+// Rotation of y = R x (dir = +1) or y = R^T x (dir = -1) over the axes of a
+// video.  table: (cos, sin) per axis, position and pair, the axis's first
+// entry at tab_off; half: pairs per axis.
+struct RopeTable {
+    const float2* table;
+    int tab_off[3], half[3];
+    int frames, height, width;
+    int halves;                // pairing: 0 adjacent channels, 1 halves of the axis
+};
+hipError_t launch_rope(const RopeTable& t, const Strided& x, const Strided& y, int B, int H, int L, int d, int text,
+                       int first, const int32_t* starts, bool backward, hipStream_t s);
+
+// The caller's cache.
+struct CacheView {
+    uint8_t *k, *v;            // [B, H, cap, d]
+    float *ks, *vs;            // [B, H, n]
+    int B, H, cap, d, block, n, format;
+};
+hipError_t launch_cache_write(const CacheView& c, const Strided& k, const Strided& v, int L, int first,
+                              const int32_t* starts, const int32_t* counts, hipStream_t s);
+hipError_t launch_cache_read(const CacheView& c, const Strided& k, const Strided& v, int L, int first,
+                             const int32_t* starts, const int32_t* counts, hipStream_t s);
+
+// Attention over the cache.  ws: at least cache_attn_ws_bytes.
+size_t cache_attn_ws_bytes(int B, int H, int d, int block, int Hq, int Lq, int max_len);
+hipError_t launch_cache_attn(const CacheView& c, const uint16_t* q, int Hq, int Lq, int max_len,
+                             const int32_t* kv_len, const int32_t* kv_idx, const int32_t* kv_cnt, float scale,
+                             uint16_t* o, float* lse, void* ws, hipStream_t s);
 
 }  // namespace moddit

@@ -1,0 +1,344 @@
+"""Attention over the 8-bit cache against the definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import cached_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def M():
+    import paper_2601_11641_amd as m
+    return m
+
+
+class Filled:
+    """A cache with arbitrary codes and scales; nothing behind a sequence's
+    end or in blocks past it is a number."""
+
+    def __init__(self, M, B, H, cap, d, block, fmt, lens, seed=0, spread=1.0):
+        g = torch.Generator().manual_seed(seed)
+        self.M, self.B, self.H, self.cap, self.d, self.block, self.fmt, self.lens = M, B, H, cap, d, block, fmt, lens
+        self.shape = M.make_cache_shape(B, H, cap, d, block, fmt)
+        n = -(-cap // block)
+        self.codes, self.scales = [], []
+        for t in range(2):
+            x = torch.randn((B, H, cap, d), generator=g)
+            if fmt == R.INT8:
+                c = (x * 40).round().clamp(-127, 127).to(torch.int8).view(torch.uint8)
+                s = (0.5 + torch.rand((B, H, n), generator=g)) * (spread if t == 0 else 1.0) / 40
+            else:
+                c = (x * 100).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+                s = torch.exp2(torch.randint(-8, -5, (B, H, n), generator=g).float()) * (spread if t == 0 else 1.0)
+            for b in range(B):
+                c[b, :, lens[b]:] = 0x7f                       # e4m3: NaN; int8: the largest
+                s[b, :, -(-lens[b] // block):] = math.nan
+            self.codes.append(c)
+            self.scales.append(s)
+        self.dev = [t.cuda() for t in self.codes + self.scales]
+        self.ref = M.make_cache(*self.dev)
+        k, v = (R.dequant_by(c, s, fmt, block) for c, s in zip(self.codes, self.scales))
+        self.kv = (k, v)
+
+    def lists(self, Hq, nq, max_len, seed, keep=0.5):
+        """Kept blocks per row, some rows empty, in any order, with entries
+        that have to be skipped among them."""
+        g = torch.Generator().manual_seed(seed)
+        n = -(-max_len // self.block)
+        idx = torch.randint(-2 ** 31, 2 ** 31 - 1, (self.B, Hq, nq, n), generator=g).int()
+        cnt = torch.zeros((self.B, Hq, nq), dtype=torch.int32)
+        kept = []
+        for b in range(self.B):
+            kept.append([])
+            for h in range(Hq):
+                kept[-1].append([])
+                for i in range(nq):
+                    js = torch.randperm(n, generator=g)
+                    js = js[torch.rand(n, generator=g) < (0.0 if (h + i) % 5 == 4 else keep)].tolist()
+                    row = list(js)
+                    if len(row) < n and (h + i) % 3 == 0:
+                        row.insert(len(row) // 2, [-1, n, 2 ** 31 - 1][i % 3])
+                    idx[b, h, i, :len(row)] = torch.tensor(row, dtype=torch.int32)
+                    cnt[b, h, i] = len(row)
+                    kept[-1][-1].append(js)
+        return idx, cnt, kept
+
+    def run(self, q, max_len, kv_len=None, idx=None, cnt=None, scale=0.0, stream=None, workspace=None):
+        B, Hq, Lq, d = q.shape
+        o = torch.full(q.shape, 7.0, dtype=torch.bfloat16).cuda()
+        lse = torch.full((B, Hq, Lq), 7.0).cuda()
+        args = [None if t is None else t.cuda() for t in (kv_len, idx, cnt)]
+        self.M.mod_cache_attn_fwd(self.shape, self.ref, q.cuda(), max_len, *args, scale, o, lse, workspace,
+                                  0 if workspace is None else workspace.numel(), stream)
+        return o, lse
+
+
+def check(f, q, o, lse, lens, scale, kept=None):
+    want, wl, eo, el = R.attention(q, *f.kv, lens, f.block, scale, kept)
+    o, lse = o.cpu().double(), lse.cpu().double()
+    assert torch.equal(lse == -math.inf, wl == -math.inf)
+    none = wl == -math.inf
+    assert torch.all(o[none] == 0)
+    assert torch.all(((lse - wl).abs() <= el)[~none]), ((lse - wl).abs() / el)[~none].max()
+    assert torch.all(((o - want).abs() <= eo)[~none]), ((o - want).abs() / eo.clamp(min=1e-30))[~none].max()
+
+
+def queries(B, Hq, Lq, d, seed, amp=1.0):
+    return (amp * torch.randn((B, Hq, Lq, d), generator=torch.Generator().manual_seed(seed))).bfloat16()
+
+
+FORMS = [(d, block, fmt) for d in (64, 128) for block in (64, 128) for fmt in (R.E4M3, R.INT8)]
+
+
+@pytest.mark.parametrize("d,block,fmt", FORMS)
+@pytest.mark.parametrize("Lq", [1, 3, 16, 17, 40, 65, 130])
+def test_all_blocks(M, d, block, fmt, Lq):
+    """Grouped heads, sequences of different lengths: none, one token, inside
+    and at the ends of steps and blocks."""
+    lens = [0, 1, 31, 32, 33, 128, 200, 300]
+    f = Filled(M, 8, 2, 300, d, block, fmt, lens, seed=Lq)
+    q = queries(8, 4, Lq, d, Lq)
+    o, lse = f.run(q, 300, torch.tensor(lens, dtype=torch.int32))
+    check(f, q, o, lse, lens, d ** -0.5)
+
+
+@pytest.mark.parametrize("d,block,fmt", FORMS)
+@pytest.mark.parametrize("Lq", [1, 20, 64, 129, 300])
+def test_lists(M, d, block, fmt, Lq):
+    lens = [500, 333, 7]
+    f = Filled(M, 3, 2, 500, d, block, fmt, lens, seed=Lq)
+    q = queries(3, 4, Lq, d, Lq + 1)
+    idx, cnt, kept = f.lists(4, -(-Lq // block), 500, Lq)
+    o, lse = f.run(q, 500, torch.tensor(lens, dtype=torch.int32), idx, cnt, 0.3)
+    check(f, q, o, lse, lens, 0.3, kept)
+
+
+@pytest.mark.parametrize("Lq,Hq,lists", [(1, 2, False), (1, 16, False), (5, 2, True), (40, 8, False), (200, 2, False),
+                                         (200, 2, True), (700, 2, True)])
+@pytest.mark.parametrize("d,fmt", [(128, R.INT8), (64, R.E4M3)])
+def test_long_walks_are_split(M, Lq, Hq, lists, d, fmt):
+    """Few rows over a long cache: parts of a walk, joined; keys whose scores
+    grow along it, so that the running maximum moves."""
+    cap, block = 9001, 128
+    f = Filled(M, 1, 2, cap, d, block, fmt, [cap], seed=3, spread=2.0)
+    q = queries(1, Hq, Lq, d, 5, 2.0)
+    idx = cnt = kept = None
+    if lists:
+        idx, cnt, kept = f.lists(Hq, -(-Lq // block), cap, 9, 0.6)
+    assert M.mod_cache_attn_workspace_bytes(f.shape, Hq, Lq, cap) > 0
+    o, lse = f.run(q, cap, None, idx, cnt)
+    check(f, q, o, lse, [cap], d ** -0.5, kept)
+    again = f.run(q, cap, None, idx, cnt)
+    assert torch.equal(again[0], o) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("Lq", [1, 70, 200])
+def test_large_scores_and_empty_parts(M, Lq):
+    """Scores up to a few hundred, and sequences much shorter than the cut-up
+    length, which leave parts without a token."""
+    lens, d, block = [40, 4000, 1, 0], 128, 64
+    f = Filled(M, 4, 1, 4000, d, block, R.INT8, lens, seed=3, spread=12.0)
+    q = queries(4, 2, Lq, d, 5, 3.0)
+    o, lse = f.run(q, 4000, torch.tensor(lens, dtype=torch.int32))
+    check(f, q, o, lse, lens, d ** -0.5)
+
+
+def test_empty_cache_and_shorter_length(M):
+    f = Filled(M, 2, 2, 200, 64, 64, R.E4M3, [150, 150])
+    q = queries(2, 2, 5, 64, 1)
+    o, lse = f.run(q, 0)
+    assert torch.all(o == 0) and torch.all(lse == -math.inf)
+    o, lse = f.run(q, 150)
+    check(f, q, o, lse, [150, 150], 0.125)
+    # lengths of the device past max_len and below zero
+    o, lse = f.run(q, 100, torch.tensor([2 ** 31 - 1, -5], dtype=torch.int32))
+    check(f, q, o, lse, [100, 0], 0.125)
+
+
+@pytest.mark.parametrize("Lq", [1, 150])
+@pytest.mark.parametrize("lists", [False, True])
+def test_infinities_and_nan(M, Lq, lists):
+    """A NaN scale reaches the rows that read its block and no others; an
+    infinite query gives NaN in its own row alone."""
+    d, block, n = 128, 64, 6
+    f = Filled(M, 1, 2, n * block, d, block, R.INT8, [n * block])
+    q = queries(1, 2, Lq, d, 1)
+    nq = -(-Lq // block)
+    if not lists:
+        o0, lse0 = f.run(q, n * block)
+        q[0, 1, 0, 3] = math.inf
+        o, lse = f.run(q, n * block)
+        assert not o[0, 1, 0].isfinite().any() and lse[0, 1, 0].isnan()
+        o[0, 1, 0], lse[0, 1, 0] = o0[0, 1, 0], lse0[0, 1, 0]
+        assert torch.equal(o, o0) and torch.equal(lse, lse0)
+        return
+    for t in (2, 3):
+        idx = torch.zeros((1, 2, nq, n), dtype=torch.int32)
+        idx[0, 0] = torch.arange(n)
+        idx[0, 1] = torch.tensor([0, 1, 3, 4, 5, 2])
+        cnt = torch.tensor([6, 5], dtype=torch.int32).view(1, 2, 1).expand(1, 2, nq).contiguous()
+        f.dev[t][0, :, 2] = math.nan           # block 2: head 0 reads it, head 1 does not
+        o, lse = f.run(q, n * block, None, idx, cnt)
+        assert o[0, 0].isnan().all() and o[0, 1].isfinite().all() and lse[0, 1].isfinite().all()
+        assert lse[0, 0].isnan().all() == (t == 2)
+        f.dev[t][0, :, 2] = 1.0
+
+
+def test_offsets_past_32_bits(M):
+    """A cache of 5 GB per tensor: its last head's last tokens, written, read
+    and attended to over lists and over a long walk."""
+    B, H, cap, d, block, L = 1, 5, 1 << 23, 128, 128, 300
+    shape = M.make_cache_shape(B, H, cap, d, block, R.E4M3)
+    c = M.Cache(shape)
+    c.k.zero_()
+    c.v.zero_()
+    c.k_scale.zero_()
+    c.v_scale.zero_()
+    k, v = queries(B, H, L, d, 1), queries(B, H, L, d, 2)
+    M.mod_cache_write(shape, c.ref, k.cuda(), v.cuda(), cap - L)
+    kb, vb = torch.empty_like(k, device="cuda"), torch.empty_like(v, device="cuda")
+    M.mod_cache_read(shape, c.ref, kb, vb, cap - L)
+    kd, vd = kb.cpu().double(), vb.cpu().double()
+    assert torch.all((kd - k.double()).abs() <= 2.0 ** -4 * k.double().abs() + 2.0 ** -9 * 2.0 ** -6)
+    assert torch.all((vd - v.double()).abs() <= 2.0 ** -4 * v.double().abs() + 2.0 ** -9 * 2.0 ** -6)
+    n, first = cap // block, (cap - L) // block
+    q = queries(B, H, 2, d, 3)
+    idx = torch.full((B, H, 1, n), -1, dtype=torch.int32)
+    idx[..., :3] = torch.arange(first, first + 3)
+    cnt = torch.full((B, H, 1), 3, dtype=torch.int32)
+    o, lse = torch.empty_like(q, device="cuda"), torch.empty((B, H, 2)).cuda()
+    M.mod_cache_attn_fwd(shape, c.ref, q.cuda(), cap, None, idx.cuda(), cnt.cuda(), 0.0, o, lse)
+    at = 3 * block - L     # zero rows of the first listed block
+    pad = torch.zeros((B, H, at, d), dtype=torch.float64)
+    class F:
+        kv = (torch.cat([pad, kd], 2), torch.cat([pad, vd], 2))
+    F.block = block
+    check(F, q, o, lse, [3 * block], d ** -0.5)
+    # every token: the zeros in front have score 0
+    M.mod_cache_attn_fwd(shape, c.ref, q.cuda(), cap, None, None, None, 0.0, o, lse)
+    s = q.double() @ kd.transpose(2, 3) * d ** -0.5
+    w = torch.exp(s)
+    total = w.sum(-1) + (cap - L)
+    want = (w @ vd) / total[..., None]
+    assert torch.all((lse.cpu().double() - total.log()).abs() <= 1e-4)   # sums of 2^23 ones in parts: 2^-24 each step
+    err = (o.cpu().double() - want).abs()
+    assert torch.all(err <= 2 * R.BF16 * (want.abs() + (w @ vd.abs()) / total[..., None]) + 1e-4 * want.abs())
+
+
+def test_other_stream_and_no_lse(M):
+    f = Filled(M, 2, 2, 5000, 128, 128, R.INT8, [5000, 5000], seed=4)
+    q = queries(2, 2, 1, 128, 2)
+    o0, _ = f.run(q, 5000)
+    qd, o = q.cuda(), torch.empty_like(q, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    M.mod_cache_attn_fwd(f.shape, f.ref, qd, 5000, None, None, None, 0.0, o, None, stream=side)
+    trash = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")   # would take the workspace's place
+    side.synchronize()
+    assert torch.equal(o, o0) and trash[0] == 255
+
+
+def test_captured_and_replayed(M):
+    """A captured step over lengths of the device, in two graphs with a
+    workspace each."""
+    B, H, Hq, cap, d = 2, 2, 8, 4096, 128
+    f = Filled(M, B, H, cap, d, 128, R.E4M3, [cap, cap], seed=5)
+    need = M.mod_cache_attn_workspace_bytes(f.shape, Hq, 1, cap)
+    assert need > 0
+    states = []
+    for s in range(2):
+        q = queries(B, Hq, 1, d, s).cuda()
+        st = dict(q=q, o=torch.empty_like(q), lse=torch.empty((B, Hq, 1)).cuda(),
+                  len=torch.tensor([5, 7], dtype=torch.int32).cuda(),
+                  ws=torch.full((need,), 255, dtype=torch.uint8).cuda(), g=torch.cuda.CUDAGraph())
+        def call(st=st):
+            M.mod_cache_attn_fwd(f.shape, f.ref, st["q"], cap, st["len"], None, None, 0.0, st["o"], st["lse"], st["ws"],
+                                 need)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            call()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(st["g"]):
+            call()
+        states.append(st)
+    for t in range(4):
+        lens = [[5, 7], [4096, 1], [0, 3000], [129, 4000]][t]
+        for s, st in enumerate(states):
+            q = queries(B, Hq, 1, d, 10 * t + s)
+            st["q"].copy_(q)
+            st["len"].copy_(torch.tensor(lens, dtype=torch.int32))
+            st["ref"] = f.run(q, cap, torch.tensor(lens, dtype=torch.int32))
+        torch.cuda.synchronize()
+        for st in states:
+            st["g"].replay()
+        torch.cuda.synchronize()
+        for st in states:
+            assert torch.equal(st["o"], st["ref"][0]) and torch.equal(st["lse"], st["ref"][1])
+
+
+@pytest.mark.parametrize("fmt", [R.E4M3, R.INT8])
+def test_layer_of_a_stream_of_frames(M, fmt):
+    """The layer as a streamed video runs it: every chunk of frames is rotated,
+    written and attended from, over all blocks and over predicted lists, with
+    the layer's own predictor; each stage against 64 bits on its inputs."""
+    H, d, block, grid, chunk = 2, 64, 64, (6, 9, 12), 2
+    hw = grid[1] * grid[2]
+    total, Lc = grid[0] * hw, chunk * hw
+    g = torch.Generator().manual_seed(7)
+    qkv = torch.randn((1, total, 3, H, d), generator=g).bfloat16()
+    q, k, v = (qkv[:, :, t].transpose(1, 2) for t in range(3))
+    dims, pos = (16, 24, 24), torch.arange(total)[None]
+    qr, kr = (R.rope(x, dims, grid, 1e4, False, pos) for x in (q, k))
+    dev = qkv.cuda()
+    rope = M.Rope(M.make_rope_params(d, dims, grid))
+    cs = M.make_cache_shape(1, H, total, d, block, fmt)
+    c = M.Cache(cs)
+    codes = [torch.zeros((1, H, total, d), dtype=torch.uint8) for _ in range(2)]
+    scales = [torch.zeros((1, H, c.n)) for _ in range(2)]
+    allq, allk = (torch.empty((1, H, total, d), dtype=torch.bfloat16).cuda() for _ in range(2))
+    for at in range(0, total, Lc):
+        shape = M.make_shape(1, H, Lc, d, block, hw)
+        part = [dev[:, at:at + Lc, t].transpose(1, 2) for t in range(3)]
+        qd, kd = (torch.empty((1, H, Lc, d), dtype=torch.bfloat16).cuda() for _ in range(2))
+        M.mod_rope_fwd(rope.handle, shape, part[0], qd, at)
+        M.mod_rope_fwd(rope.handle, shape, part[1], kd, at)
+        for got, want, x in ((qd, qr, q), (kd, kr, k)):
+            w = want[:, :, at:at + Lc]
+            top = x[:, :, at:at + Lc].double().abs().amax(-1, keepdim=True)
+            assert torch.all((got.cpu().double() - w).abs() <= R.BF16 * w.abs() + 8.1 * R.F32 * top)
+        M.mod_cache_write(cs, c.ref, kd, part[2], at)
+        R.write(codes[0], scales[0], kd.cpu(), block, fmt, [at], [Lc])
+        R.write(codes[1], scales[1], part[2].cpu(), block, fmt, [at], [Lc])
+        o, lse = torch.empty_like(qd), torch.empty((1, H, Lc)).cuda()
+        M.mod_cache_attn_fwd(cs, c.ref, qd, at + Lc, None, None, None, 0.0, o, lse)
+        class F:
+            kv = tuple(R.dequant_by(a, b, fmt, block) for a, b in zip(codes, scales))
+        F.block = block
+        check(F, qd.cpu(), o, lse, [at + Lc], d ** -0.5)
+        allq[:, :, at:at + Lc], allk[:, :, at:at + Lc] = qd, kd
+    # the whole sequence over the predictor's lists, as the bf16 attention has them
+    shape = M.make_shape(1, H, total, d, block, hw)
+    stats = M.Stats(shape, M.make_params(warmup_m=1))
+    n = stats.n
+    idx = torch.full((1, H, n, n), -1, dtype=torch.int32).cuda()
+    cnt = torch.zeros((1, H, n), dtype=torch.int32).cuda()
+    M.mod_collect_stats(stats.handle, allq, allk, 1)
+    M.mod_predict_block_mask(stats.handle, allq, allk, 2, M.make_budget("topk", density=0.4), idx, cnt)
+    o, lse = torch.empty_like(allq), torch.empty((1, H, total)).cuda()
+    M.mod_cache_attn_fwd(cs, c.ref, allq, total, None, idx, cnt, 0.0, o, lse)
+    ic, cc = idx.cpu(), cnt.cpu()
+    kept = [[[ic[0, h, i, :cc[0, h, i]].tolist() for i in range(n)] for h in range(H)]]
+    check(F, allq.cpu(), o, lse, [total], d ** -0.5, kept)
+    # and next to the bf16 attention over what the cache stands for: the same sums
+    kb, vb, o2 = (torch.empty_like(allq) for _ in range(3))
+    M.mod_cache_read(cs, c.ref, kb, vb)
+    lse2 = torch.empty_like(lse)
+    M.mod_block_sparse_attn_fwd(shape, allq, kb, vb, idx, cnt, 0.0, o2, lse2)
+    if fmt == R.E4M3:      # code * scale is a bf16 number: the same K and V
+        w, wl, eo, el = R.attention(allq.cpu(), *F.kv, [total], block, d ** -0.5, kept)
+        assert torch.all((o.double() - o2.double()).cpu().abs() <= 2 * eo)
+        assert torch.all((lse.double() - lse2.double()).cpu().abs() <= 2 * el)
