@@ -29,14 +29,21 @@
 namespace moddit {
 namespace {
 
+typedef __bf16 bf16x2 __attribute__((__vector_size__(2 * sizeof(__bf16))));
 typedef __bf16 bf16x8 __attribute__((__vector_size__(8 * sizeof(__bf16))));
+typedef short s16x4 __attribute__((__vector_size__(4 * sizeof(short))));
+typedef short s16x8 __attribute__((__vector_size__(8 * sizeof(short))));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4_t;
+typedef __attribute__((address_space(3))) const uint4 lds_u4_t;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kXcds = 8;
 constexpr int kStep = 32;          // tokens of a wave's step
+constexpr float kSumLimit = 256.0f; // bound on a lane's probability sum per unit while its maximum is kept
 
 struct AttnArgs {
     const uint16_t* q;
@@ -47,10 +54,12 @@ struct AttnArgs {
     float* lse;
     float* part;               // C > 1: O / l of every item, then its log2-sum-exp2
     int B, Hq, H, Lq, cap, ncap, max_len, n, nq, block;
+    int shift;                 // block = 1 << shift
+    int group;                 // query heads per key/value head
     int tiles;                 // row tiles per head and query block (lists) or key/value head
     int heads;                 // heads that items count: Hq with lists, H without
     int C;                     // parts of a walk
-    long units;                // B * heads * (lists: nq) * tiles
+    int units;                 // B * heads * (lists: nq) * tiles
     float c2;                  // scale * log2(e)
 };
 
@@ -85,6 +94,11 @@ __device__ __forceinline__ uint32_t column_pair(uint32_t a, uint32_t b) {
     }
 }
 
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const bf16x2 r = {static_cast<__bf16>(lo), static_cast<__bf16>(hi)};   // one instruction
+    return __builtin_bit_cast(uint32_t, r);
+}
+
 // max / sum over the four lanes that hold a query row's tokens (16 apart)
 __device__ __forceinline__ float max4(float x) {
     x = fmaxf(x, __shfl_xor(x, 16));
@@ -106,18 +120,18 @@ struct Rows {
     int count;                 // rows of the tile that exist
 };
 template <int ROWS, bool LISTS>
-__device__ __forceinline__ Rows rows_of(const AttnArgs& a, long u) {
+__device__ __forceinline__ Rows rows_of(const AttnArgs& a, int u) {
     Rows r;
-    const int t = (int)(u % a.tiles);
+    const int t = u % a.tiles;
     u /= a.tiles;
     r.i = 0;
     if (LISTS) {
-        r.i = (int)(u % a.nq);
+        r.i = u % a.nq;
         u /= a.nq;
     }
-    r.head = (int)(u % a.heads);
-    r.b = (int)(u / a.heads);
-    const int group = a.Hq / a.H;
+    r.head = u % a.heads;
+    r.b = u / a.heads;
+    const int group = a.group;
     r.kv = LISTS ? r.head / group : r.head;
     const int all = LISTS ? min(a.block, a.Lq - r.i * a.block) : group * a.Lq;
     r.row0 = (LISTS ? ((long)r.b * a.Hq + r.head) * a.Lq + (long)r.i * a.block
@@ -136,17 +150,16 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
     __shared__ float obuf[4][16][LDO];
     __shared__ float mbuf[4][ROWS], lbuf[4][ROWS];
 
-    const long total = a.units * a.C;
+    const int total = a.units * a.C;
     // consecutive work-groups go to the dies in turn: a die takes one stretch of
     // the items, whose neighbours read the same tokens
-    const long per = (total + kXcds - 1) / kXcds;
-    const long w = (long)(blockIdx.x % kXcds) * per + blockIdx.x / kXcds;
-    if (blockIdx.x / kXcds >= per || w >= total) return;
+    const int per = (total + kXcds - 1) / kXcds;
+    const int w = (int)(blockIdx.x % kXcds) * per + (int)(blockIdx.x / kXcds);
+    if ((int)(blockIdx.x / kXcds) >= per || w >= total) return;
     // order: head, part of the walk, then the tiles that share it
-    const long tiles = (LISTS ? (long)a.nq : 1) * a.tiles;
-    const long hb = w / (tiles * a.C);
-    const int part = (int)(w / tiles % a.C);
-    const long unit = hb * tiles + w % tiles;
+    const int tiles = (LISTS ? a.nq : 1) * a.tiles;
+    const int hb = w / (tiles * a.C), rest = w % (tiles * a.C);
+    const int part = rest / tiles, unit = hb * tiles + rest % tiles;
     const Rows r = rows_of<ROWS, LISTS>(a, unit);
     if (r.count <= 0) return;           // a tile past a short query block
 
@@ -158,17 +171,15 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
     const uint8_t* vp = a.v + hk * a.cap * D + VF * l16;
     const float* ksp = a.ks + hk * a.ncap;
     const float* vsp = a.vs + hk * a.ncap;
-    const int per_block = a.block / kStep;
+    const int ps = a.shift - 5;         // steps per block: 1 << ps
     const int32_t* list = nullptr;
-    long steps;
+    int steps = (len + kStep - 1) / kStep;
     if (LISTS) {
         const long lrow = ((long)r.b * a.Hq + r.head) * a.nq + r.i;
         list = a.idx + lrow * a.n;
-        steps = (long)min(max(a.cnt[lrow], 0), a.n) * per_block;
-    } else {
-        steps = (len + kStep - 1) / kStep;
+        steps = min(max(a.cnt[lrow], 0), a.n) << ps;
     }
-    const int s0 = (int)(steps * part / a.C), s1 = (int)(steps * (part + 1) / a.C);
+    const int s0 = (int)((long)steps * part / a.C), s1 = (int)((long)steps * (part + 1) / a.C);
 
     // Q as the second operand: row l16 of tile rt, the channels that a lane of
     // group g loads of K
@@ -198,8 +209,8 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
     // first token of step s, or -1 where there is none
     auto token_of = [&](int s) {
         if (!LISTS) return s * kStep;
-        const int j = list[s / per_block];
-        const int t = j * a.block + s % per_block * kStep;
+        const int j = list[s >> ps];
+        const int t = j * a.block + (s & ((1 << ps) - 1)) * kStep;
         return (j < 0 || j >= a.n || t >= len) ? -1 : t;
     };
     uint4 kw[2][KC];
@@ -224,8 +235,8 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
                 vw[e][0] = *reinterpret_cast<const uint32_t*>(vp + row);
             }
         }
-        ksc = ksp[t0 / a.block];
-        vsc = vsp[t0 / a.block];
+        ksc = ksp[t0 >> a.shift];
+        vsc = vsp[t0 >> a.shift];
     };
 
     for (int s = s0 + wave; s < s1; s += 4) {
@@ -330,21 +341,460 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
             out[e] = (obuf[0][orow][ch + e] + obuf[1][orow][ch + e] + obuf[2][orow][ch + e] + obuf[3][orow][ch + e]) * inv;
         const float lse2 = sum == 0.0f ? -INFINITY : tt + __builtin_amdgcn_logf(sum);   // log2
         if (a.C > 1) {
-            const long slot = (unit * a.C + part) * ROWS + tr;
+            const long slot = ((long)unit * a.C + part) * ROWS + tr;
             float* po = a.part + slot * D + ch;
 #pragma unroll
             for (int e = 0; e < W; e += 4)
                 *reinterpret_cast<float4*>(po + e) = make_float4(out[e], out[e + 1], out[e + 2], out[e + 3]);
-            if (tid % 16 == 0) (a.part + a.units * a.C * ROWS * D)[slot] = lse2;
+            if (tid % 16 == 0) (a.part + (long)a.units * a.C * ROWS * D)[slot] = lse2;
         } else if (tr < r.count) {
             uint32_t* po = reinterpret_cast<uint32_t*>(a.o + (r.row0 + tr) * D + ch);
 #pragma unroll
             for (int e = 0; e < W; e += 2)
-                po[e / 2] = (uint32_t)__builtin_bit_cast(uint16_t, static_cast<__bf16>(out[e])) |
-                            ((uint32_t)__builtin_bit_cast(uint16_t, static_cast<__bf16>(out[e + 1])) << 16);
+                po[e / 2] = pack_bf16(out[e], out[e + 1]);
             if (a.lse && tid % 16 == 0) a.lse[r.row0 + tr] = lse2 * kLn2;
         }
         __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------
+// tile_kernel: tiles of 32 WAVES query rows of a head, for calls with many rows.
+// The work-group brings the walk's tokens into LDS as bf16, 64 at a time (a
+// "unit"), so a code is converted once for all rows of the tile; a wave owns 32
+// rows.  It works on halves of a unit (32 tokens) as a pipeline of three:
+//   scores    S^T (32 tokens x 32 rows) = K Q^T of one half,
+//   softmax   of the half before it (P stays in the lanes that the product
+//             wants it in),
+//   product   O^T += V^T P^T of the half before that,
+// with v_mfma_f32_32x32x16_bf16; V^T comes from the row-major tile through
+// transposing LDS reads.  A wave issues an instruction every eight cycles at
+// most and a matrix instruction takes 32, so the matrix instructions of a half
+// ("slots") are spaced out by its vector instructions: the softmax, and the
+// conversion of the codes of the next unit, which were loaded one unit earlier.
+// K and V tiles are double-buffered, V one unit behind K: one barrier a unit.
+// ---------------------------------------------------------------------------
+constexpr int kUnit = 64;
+
+template <class F, int... I>
+__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+    static_for_impl(f, std::make_integer_sequence<int, N>{});
+}
+
+// A value that all lanes share, in a scalar register.
+__device__ __forceinline__ float uniform(float x) {
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
+
+// What the softmax needs to know of a unit.
+struct Unit {
+    float sc;       // scale * s_k, in units of log 2
+    float lv, ivs;  // log2 s_v and 1 / s_v (0 and 1 where the scale goes into the values instead)
+    int valid;      // tokens of the unit that exist
+};
+
+template <int D, int FMT, bool LISTS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
+    constexpr int ROWS = 32 * WAVES;
+    constexpr int DT = D / 32, KK = D / 16;
+    constexpr int SLOTS = KK + 2 * DT;           // matrix instructions of a half
+    // LDS rows of K are 16 bytes longer than their 2 D bytes, so that the 16 rows
+    // that an operand read takes at once lie in different banks; those of V 64
+    // bytes, for the 4 rows of 64 bytes of a transposing read.  (A swizzle
+    // instead would need an address register per operand of a half.)
+    constexpr int KROW = 2 * D + 16, VROW = 2 * D + 64;
+    constexpr int KTILE = kUnit * KROW, VTILE = kUnit * VROW;
+    constexpr int CPT = D / WAVES;               // codes of a tile that a thread brings: in pieces of
+    constexpr int PIECE = CPT < 16 ? CPT : 16;   // one load,
+    constexpr int NP = CPT / PIECE;              // each of a token TPP after the other's
+    constexpr int TPR = D / PIECE, TPP = 64 * WAVES / TPR;
+    constexpr int PW = PIECE / 4;                // dwords of a piece
+    // With eight waves, which alone fill a compute unit, three buffers: the
+    // barrier lies between the halves, behind the conversion of both tiles, and
+    // no operand read waits for it.  With four, two work-groups share the unit
+    // and cover each other; two buffers each, and the barrier at the unit's end.
+    constexpr int NB = WAVES == 8 ? 3 : 2;
+    __shared__ __align__(1024) char lds[NB * (KTILE + VTILE)];
+
+    const int total = a.units * a.C, per = (total + kXcds - 1) / kXcds;
+    const int w = (int)(blockIdx.x % kXcds) * per + (int)(blockIdx.x / kXcds);
+    if ((int)(blockIdx.x / kXcds) >= per || w >= total) return;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int qw = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l32 = lane & 31, h = lane >> 5;
+    const int tiles = (LISTS ? a.nq : 1) * a.tiles;
+    const int hb = w / (tiles * a.C), rest = w % (tiles * a.C);
+    const int part = rest / tiles, unit = hb * tiles + rest % tiles;
+    const Rows r = rows_of<ROWS, LISTS>(a, unit);
+    if (r.count <= 0) return;                    // a tile past a short query block
+
+    const int len = clamp_len(a, r.b);
+    const size_t hk = (size_t)r.b * a.H + r.kv;
+    const uint8_t* kcodes = a.k + hk * a.cap * D;
+    const uint8_t* vcodes = a.v + hk * a.cap * D;
+    const float* ksp = a.ks + hk * a.ncap;
+    const float* vsp = a.vs + hk * a.ncap;
+    const int us = a.shift - 6;                  // units per block: 1 << us
+    const int32_t* list = nullptr;
+    int steps = (len + kUnit - 1) / kUnit;
+    if (LISTS) {
+        const long lrow = ((long)r.b * a.Hq + r.head) * a.nq + r.i;
+        list = a.idx + lrow * a.n;
+        steps = len > 0 ? min(max(a.cnt[lrow], 0), a.n) << us : 0;
+    }
+    const int u0 = (int)((long)steps * part / a.C);
+    const int T = __builtin_amdgcn_readfirstlane((int)((long)steps * (part + 1) / a.C) - u0);   // units of this item
+
+    const int row = 32 * qw + l32;               // the lane's row of the tile
+    bf16x8 qreg[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (row < r.count) x = *reinterpret_cast<const uint4*>(a.q + (r.row0 + row) * D + 16 * kk + 8 * h);
+        qreg[kk] = __builtin_bit_cast(bf16x8, x);
+    }
+    f32x16 oacc[DT], sacc[2];
+    u32x4 pf[2][2];                              // P of either half, pairs of bf16
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) oacc[dt] = f32x16{};
+    float m = -INFINITY, l = 0.0f;
+
+    // LDS addresses of the operands in the first buffers
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)lds;
+    const int s16 = lane & 15;
+    const uint32_t kad = lds0 + (uint32_t)(l32 * KROW + 16 * h);
+    const uint32_t vad = lds0 + (uint32_t)(NB * KTILE + (4 * h + (s16 >> 2)) * VROW + 32 * (lane >> 4 & 1) + 8 * (s16 & 3));
+
+    // staging: thread tid brings a piece of a token's codes, one or two 16-byte
+    // chunks of its LDS row
+    const int scol = tid % TPR, srow = tid / TPR;
+    char* const kst = lds + srow * KROW + 2 * PIECE * scol;
+    char* const vst = lds + NB * KTILE + srow * VROW + 2 * PIECE * scol;
+    uint32_t kr[NP][PW], vr[NP][PW];
+    auto entry_of = [&](int u) __attribute__((always_inline)) { return LISTS ? list[(u0 + u) >> us] : 0; };
+    // first token of unit u, whose list entry is j; -1: nothing to read
+    auto token_of = [&](int u, int j) __attribute__((always_inline)) {
+        u += u0;
+        if (!LISTS) return u * kUnit;
+        j = __builtin_amdgcn_readfirstlane(j);
+        const int t = j * a.block + (u & ((1 << us) - 1)) * kUnit;
+        return (j < 0 || j >= a.n || t >= len) ? -1 : t;
+    };
+    auto load = [&](const uint8_t* p, int t0, uint32_t (&x)[NP][PW]) __attribute__((always_inline)) {
+        if (t0 < 0) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int q = 0; q < PW; ++q) x[i][q] = 0;
+            return;
+        }
+        const uint8_t* base = p + (size_t)t0 * D;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int t = min(srow + TPP * i, len - 1 - t0);       // rows past the end: masked
+            const uint32_t off = (uint32_t)(t * D + PIECE * scol);
+            if constexpr (PW == 4) {
+                const uint4 v = *reinterpret_cast<const uint4*>(base + off);
+                x[i][0] = v.x, x[i][1] = v.y, x[i][2] = v.z, x[i][3] = v.w;
+            } else {
+                const uint2 v = *reinterpret_cast<const uint2*>(base + off);
+                x[i][0] = v.x, x[i][1] = v.y;
+            }
+        }
+    };
+    auto fetch_scales = [&](int t0, float& ks, float& vs) __attribute__((always_inline)) {
+        ks = vs = 1.0f;
+        if (t0 >= 0) {
+            ks = ksp[t0 >> a.shift];
+            vs = vsp[t0 >> a.shift];
+        }
+    };
+    // pair q of the thread's codes; after a chunk's last pair the chunk goes to LDS
+    // (`to`: the thread's place in the buffer, whose rows are ROW bytes apart)
+    using No = std::false_type;
+    using Yes = std::true_type;
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    using KR = std::integral_constant<int, KROW>;
+    using VR = std::integral_constant<int, VROW>;
+    uint32_t kconv[4], vconv[4];
+    auto convert = [&](auto q_tag, auto row_tag, uint32_t (&x)[NP][PW], char* to, uint32_t (&conv)[4])
+                       __attribute__((always_inline)) {
+        constexpr int Q = decltype(q_tag)::value, I = Q / (2 * PW), W = Q / 2 % PW, ROW = decltype(row_tag)::value;
+        asm volatile("" : "+v"(x[I][W]));        // (keeps the conversion in its slot)
+        conv[Q % 4] = bf16_pair<FMT, Q % 2 == 1>(x[I][W]);
+        asm volatile("" : "+v"(conv[Q % 4]));
+        if constexpr (Q % 4 == 3)
+            *reinterpret_cast<uint4*>(to + TPP * I * ROW + 16 * (Q / 4 % (PW / 2))) =
+                make_uint4(conv[0], conv[1], conv[2], conv[3]);
+    };
+    constexpr int PAIRS = CPT / 2;               // pairs of codes per thread and tile
+    // V whose scale cannot stand in the exponent (0, NaN, extreme): into the values
+    auto stage_scaled = [&](char* to, float s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int c = 0; c < PW / 2; ++c) {
+                uint32_t out[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t wd = vr[i][2 * c + q / 2];
+                    const uint32_t pr = q % 2 ? bf16_pair<FMT, true>(wd) : bf16_pair<FMT, false>(wd);
+                    out[q] = pack_bf16(__uint_as_float(pr << 16) * s, __uint_as_float(pr & 0xffff0000u) * s);
+                }
+                *reinterpret_cast<uint4*>(to + TPP * i * VROW + 16 * c) = make_uint4(out[0], out[1], out[2], out[3]);
+            }
+    };
+    auto barrier = [&]() __attribute__((always_inline)) {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    // Operands that were read ahead for the next half.
+    constexpr int AHEAD = 2;                     // operand reads ahead, of either kind
+    bf16x8 nk[AHEAD];
+    s16x4 nv0[AHEAD], nv1[AHEAD];
+    auto read_k = [&](uint32_t ka, auto i) __attribute__((always_inline)) {
+        return __builtin_bit_cast(bf16x8, *(lds_u4_t*)(uintptr_t)(ka + (uint32_t)(32 * decltype(i)::value)));
+    };
+    auto read_v = [&](uint32_t va, auto i, s16x4& x0, s16x4& x1) __attribute__((always_inline)) {
+        constexpr uint32_t at = 16 * (decltype(i)::value / DT) * VROW + 64 * (decltype(i)::value % DT);
+        x0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(uintptr_t)(va + at));
+        x1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(uintptr_t)(va + at + 8 * VROW));
+    };
+    auto read_ahead = [&](uint32_t ka, uint32_t va) __attribute__((always_inline)) {
+        static_for<AHEAD>([&](auto i) __attribute__((always_inline)) {
+            nk[decltype(i)::value] = read_k(ka, i);
+            read_v(va, i, nv0[decltype(i)::value], nv1[decltype(i)::value]);
+        });
+    };
+
+    // One half: scores of the half SUB at ka (QK), softmax of the half before it,
+    // half 1 - SUB of unit `u` (SM), product of the one before that, at va (PV),
+    // and the conversion of K and V codes to kto and vto (KC, VC).  NEXT: reads
+    // the next half's first operands, at kn and vn, ahead.
+    auto half = [&](auto sub_tag, uint32_t ka, uint32_t va, auto qk_tag, auto sm_tag, auto pv_tag, auto kc_tag,
+                    auto vc_tag, auto next_tag, Unit u, char* kto, char* vto, uint32_t kn, uint32_t vn)
+                    __attribute__((always_inline)) {
+        constexpr int SUB = decltype(sub_tag)::value;
+        constexpr bool QK = decltype(qk_tag)::value, SM = decltype(sm_tag)::value, PV = decltype(pv_tag)::value;
+        constexpr bool KC = decltype(kc_tag)::value, VC = decltype(vc_tag)::value, NEXT = decltype(next_tag)::value;
+        constexpr int PS = 1 - SUB;              // the half whose softmax this is
+        constexpr int EPS = 16 / SLOTS;          // scores of a lane per slot
+        float sc = u.sc;
+        if constexpr (SM) {
+            const int lim = u.valid - 32 * PS;
+            if (lim < 32) {
+                const int mine = lim - 4 * h;
+#pragma unroll
+                for (int ii = 0; ii < 16; ++ii)
+                    sacc[PS][ii] = 8 * (ii >> 2) + (ii & 3) >= mine ? -INFINITY : sacc[PS][ii] * sc;
+                sc = 1.0f;
+            }
+        }
+        float ps0 = 0.0f, ps1 = 0.0f, off = u.lv - (m == -INFINITY ? 0.0f : m);
+        bf16x8 ak[KK];
+        s16x4 v0[2 * DT], v1[2 * DT];
+        float pr[16];
+        uint32_t pb[8];
+        // sums and pairs of scores [e0, e1), whose exponentials the slot before took
+        auto gather = [&](auto e0, auto e1) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = decltype(e0)::value; e < decltype(e1)::value; ++e) {
+                (e % 2 ? ps1 : ps0) += pr[e];
+                if (e % 2 == 1) {
+                    pb[e / 2] = pack_bf16(pr[e - 1], pr[e]);
+                    asm volatile("" : "+v"(pb[e / 2]));
+                }
+            }
+        };
+        static_for<AHEAD>([&](auto i) __attribute__((always_inline)) {
+            constexpr int I = decltype(i)::value;
+            ak[I] = nk[I];
+            v0[I] = nv0[I];
+            v1[I] = nv1[I];
+        });
+        static_for<SLOTS>([&](auto s_tag) __attribute__((always_inline)) {
+            constexpr int S = decltype(s_tag)::value, I = S / 2, J = I + AHEAD;
+            if constexpr (S % 2 == 0) {
+                if constexpr (QK)
+                    sacc[SUB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak[I], qreg[I], I == 0 ? f32x16{} : sacc[SUB], 0,
+                                                                        0, 0);
+                if constexpr (J < KK && QK) ak[J] = read_k(ka, std::integral_constant<int, J>{});
+                if constexpr (J >= KK && NEXT) nk[J - KK] = read_k(kn, std::integral_constant<int, J - KK>{});
+            } else {
+                if constexpr (PV) {
+                    const s16x8 v8 = {v0[I][0], v0[I][1], v0[I][2], v0[I][3], v1[I][0], v1[I][1], v1[I][2], v1[I][3]};
+                    oacc[I % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v8),
+                                                                           __builtin_bit_cast(bf16x8, pf[SUB][I / DT]),
+                                                                           oacc[I % DT], 0, 0, 0);
+                }
+                if constexpr (J < 2 * DT && PV) read_v(va, std::integral_constant<int, J>{}, v0[J], v1[J]);
+                if constexpr (J >= 2 * DT && NEXT)
+                    read_v(vn, std::integral_constant<int, J - 2 * DT>{}, nv0[J - 2 * DT], nv1[J - 2 * DT]);
+            }
+            if constexpr (SM) {
+                // the slot's scores, and the sums of the slot before (the empty
+                // statements keep them in their slot)
+                asm volatile("" : "+v"(off));
+                float arg[EPS];
+#pragma unroll
+                for (int e = 0; e < EPS; ++e) arg[e] = __builtin_fmaf(sacc[PS][S * EPS + e], sc, off);
+#pragma unroll
+                for (int e = 0; e < EPS; ++e) pr[S * EPS + e] = __builtin_amdgcn_exp2f(arg[e]);
+                if constexpr (S > 0)
+                    gather(std::integral_constant<int, (S - 1) * EPS>{}, std::integral_constant<int, S * EPS>{});
+#pragma unroll
+                for (int e = S * EPS; e < (S + 1) * EPS; ++e) asm volatile("" : "+v"(pr[e]));
+                asm volatile("" : "+v"(ps0), "+v"(ps1));
+            }
+            constexpr int Q0 = S * PAIRS / SLOTS, Q1 = (S + 1) * PAIRS / SLOTS;
+            static_for<Q1 - Q0>([&](auto q) __attribute__((always_inline)) {
+                using Q = std::integral_constant<int, Q0 + decltype(q)::value>;
+                if constexpr (KC) convert(Q{}, KR{}, kr, kto, kconv);
+                if constexpr (VC) convert(Q{}, VR{}, vr, vto, vconv);
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        if constexpr (SM) {
+            gather(std::integral_constant<int, 16 - EPS>{}, std::integral_constant<int, 16>{});
+            // The running maximum is kept while no lane's probabilities sum past
+            // kSumLimit; the first half and the rare others take the half's
+            // maximum and rescale.  The other rows of the wave keep theirs: a row
+            // does not depend on its neighbours.
+            int move = !(m > -INFINITY) || !((ps0 + ps1) * u.ivs <= kSumLimit);
+            if (__any(move)) {
+                float mx = -INFINITY;
+#pragma unroll
+                for (int ii = 0; ii < 16; ++ii) mx = fmaxf(mx, sacc[PS][ii] * sc);
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                move |= __shfl_xor(move, 32);
+                const float mn = move ? fmaxf(m, mx) : m;
+                const float alpha = mn == m ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) oacc[dt] *= alpha;
+                l *= alpha;
+                m = mn;
+                off = u.lv - (m == -INFINITY ? 0.0f : m);
+                ps0 = ps1 = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    pr[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[PS][e], sc, off));
+                    if (e % 2 == 1) pb[e / 2] = pack_bf16(pr[e - 1], pr[e]);
+                    (e % 2 ? ps1 : ps0) += pr[e];
+                }
+            }
+            l += (ps0 + ps1) * u.ivs;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                pf[PS][c] = u32x4{pb[4 * c], pb[4 * c + 1], pb[4 * c + 2], pb[4 * c + 3]};
+                asm volatile("" : "+v"(pf[PS][c]));
+            }
+        }
+    };
+    auto unit_of = [&](int t0, float ks, float vs) __attribute__((always_inline)) {
+        const bool plain = vs >= 0x1p-64f && vs <= 0x1p64f;
+        return Unit{uniform(ks * a.c2), uniform(plain ? __builtin_amdgcn_logf(vs) : 0.0f),
+                    uniform(plain ? __builtin_amdgcn_rcpf(vs) : 1.0f), t0 < 0 ? 0 : len - t0};
+    };
+    int tn = -1, jn = 0;                         // the next unit's first token, list entry of the one after
+
+    float ks = 1.0f, vs = 1.0f;
+    Unit before{}, now{};
+    // One unit, its K at kc and the V of the unit before at vp: its scores, the
+    // rest of the unit before, and half of its softmax.
+    int kc = 0, vp = (NB - 1) * VTILE;
+    auto iterate = [&](int t, auto first_tag) __attribute__((always_inline)) {
+        using Rest = std::bool_constant<!decltype(first_tag)::value>;
+        using Mid = std::bool_constant<NB == 3>;             // both tiles are converted in the first half
+        using End = std::bool_constant<NB != 3>;
+        const int kn = kc == (NB - 1) * KTILE ? 0 : kc + KTILE, vc = vp == (NB - 1) * VTILE ? 0 : vp + VTILE;
+        const uint32_t ka = kad + kc, va = vad + vp;
+        char* const vto = vst + vc;
+        float ksn, vsn;
+        fetch_scales(tn, ksn, vsn);
+        half(I0{}, ka, va, Yes{}, Rest{}, Rest{}, Yes{}, Mid{}, Yes{}, before, kst + kn, vto, ka + 32 * KROW,
+             va + 32 * VROW);
+        const bool special = !(vs >= 0x1p-64f && vs <= 0x1p64f);
+        if constexpr (NB == 3) {
+            if (special) stage_scaled(vto, vs);
+            barrier();
+            if (t + 1 < T) load(vcodes, tn, vr);
+        }
+        int tnn = -1;
+        if (t + 2 < T) {
+            tnn = token_of(t + 2, jn);
+            load(kcodes, tnn, kr);
+            if (t + 3 < T) jn = entry_of(t + 3);
+        }
+        half(I1{}, ka + 32 * KROW, va + 32 * VROW, Yes{}, Yes{}, Rest{}, No{}, End{}, Mid{}, now, kst, vto, kad + kn,
+             vad + vc);
+        if constexpr (NB == 2) {
+            if (special) stage_scaled(vto, vs);
+            if (t + 1 < T) load(vcodes, tn, vr);
+            barrier();
+            read_ahead(kad + kn, vad + vc);
+        }
+        before = now;
+        now = unit_of(tn, ksn, vsn);
+        vs = uniform(vsn);
+        tn = tnn;
+        kc = kn;
+        vp = vc;
+    };
+    if (T > 0) {
+        const int tc = token_of(0, entry_of(0));
+        load(kcodes, tc, kr);
+        fetch_scales(tc, ks, vs);
+        now = unit_of(tc, ks, vs);
+        vs = uniform(vs);
+        static_for<PAIRS>([&](auto q) __attribute__((always_inline)) { convert(q, KR{}, kr, kst, kconv); });
+        if (T > 1) {
+            tn = token_of(1, entry_of(1));
+            load(kcodes, tn, kr);
+        }
+        load(vcodes, tc, vr);
+        if (T > 2) jn = entry_of(2);
+        barrier();
+        read_ahead(kad, vad);                    // (the V of no unit: not used)
+        iterate(0, Yes{});
+        for (int t = 1; t < T; ++t) iterate(t, No{});
+        const uint32_t va = vad + vp;
+        half(I0{}, kad, va, No{}, Yes{}, Yes{}, No{}, No{}, Yes{}, before, kst, vst, kad, va + 32 * VROW);
+        half(I1{}, kad, va + 32 * VROW, No{}, No{}, Yes{}, No{}, No{}, No{}, before, kst, vst, kad, vad);
+    }
+
+    // the lane's channels: 32 dt + 8 gq + 4 h + 0..3 of its row
+    l += __shfl_xor(l, 32);
+    if (row >= r.count) return;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const float lse2 = l == 0.0f ? -INFINITY : m + __builtin_amdgcn_logf(l);
+    if (a.C > 1) {
+        const long slot = ((long)unit * a.C + part) * ROWS + row;
+        float* po = a.part + slot * D + 4 * h;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int gq = 0; gq < 4; ++gq)
+                *reinterpret_cast<float4*>(po + 32 * dt + 8 * gq) =
+                    make_float4(oacc[dt][4 * gq] * inv, oacc[dt][4 * gq + 1] * inv, oacc[dt][4 * gq + 2] * inv,
+                                oacc[dt][4 * gq + 3] * inv);
+        if (h == 0) (a.part + (long)a.units * a.C * ROWS * D)[slot] = lse2;
+    } else {
+        uint16_t* po = a.o + (r.row0 + row) * D + 4 * h;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int gq = 0; gq < 4; ++gq)
+                *reinterpret_cast<uint2*>(po + 32 * dt + 8 * gq) =
+                    make_uint2(pack_bf16(oacc[dt][4 * gq] * inv, oacc[dt][4 * gq + 1] * inv),
+                               pack_bf16(oacc[dt][4 * gq + 2] * inv, oacc[dt][4 * gq + 3] * inv));
+        if (a.lse && h == 0) a.lse[r.row0 + row] = lse2 * kLn2;
     }
 }
 
@@ -353,14 +803,13 @@ template <int D, int ROWS, bool LISTS>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
     constexpr int LPR = D / 4, RPG = 256 / LPR;
     const int tid = threadIdx.x;
-    const long row = (long)blockIdx.x * RPG + tid / LPR;
-    const long unit = row / ROWS;
+    const int row = (int)blockIdx.x * RPG + tid / LPR, unit = row / ROWS;
     if (unit >= a.units) return;
-    const int tr = (int)(row % ROWS), ch = tid % LPR * 4;
+    const int tr = row % ROWS, ch = tid % LPR * 4;
     const Rows r = rows_of<ROWS, LISTS>(a, unit);
     if (tr >= r.count) return;
-    const float* lse2 = a.part + a.units * a.C * ROWS * D + unit * a.C * ROWS + tr;
-    const float* po = a.part + (unit * a.C * ROWS + tr) * D + ch;
+    const float* lse2 = a.part + (long)a.units * a.C * ROWS * D + (long)unit * a.C * ROWS + tr;
+    const float* po = a.part + ((long)unit * a.C * ROWS + tr) * D + ch;
     float top = -INFINITY;
     for (int c = 0; c < a.C; ++c) top = fmaxf(top, lse2[(long)c * ROWS]);
     float sum = 0.0f;
@@ -373,50 +822,68 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
         o += w * *reinterpret_cast<const f32x4*>(po + (long)c * ROWS * D);
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    uint2 pk;
-    pk.x = (uint32_t)__builtin_bit_cast(uint16_t, static_cast<__bf16>(o[0] * inv)) |
-           ((uint32_t)__builtin_bit_cast(uint16_t, static_cast<__bf16>(o[1] * inv)) << 16);
-    pk.y = (uint32_t)__builtin_bit_cast(uint16_t, static_cast<__bf16>(o[2] * inv)) |
-           ((uint32_t)__builtin_bit_cast(uint16_t, static_cast<__bf16>(o[3] * inv)) << 16);
-    *reinterpret_cast<uint2*>(a.o + (r.row0 + tr) * D + ch) = pk;
+    *reinterpret_cast<uint2*>(a.o + (r.row0 + tr) * D + ch) =
+        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
     if (a.lse && tid % LPR == 0)
         a.lse[r.row0 + tr] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 // How a call is cut up, from its host sizes alone.
 struct Plan {
-    int rt, C;
-    int tiles, heads;
-    long units;
+    int rows;                  // rows of a tile: 16, 32, 64 (rows_kernel), 128, 256 (tile_kernel)
+    int C;                     // parts of a walk
+    int tiles, heads, units;
 };
-Plan plan_of(int B, int H, int block, int Hq, int Lq, int max_len, bool lists) {
+Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool lists) {
     Plan p;
     const int rows = lists ? std::min(block, Lq) : (int)std::min<long>((long)(Hq / H) * Lq, 1L << 30);
-    p.rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    p.tiles = (rows + 16 * p.rt - 1) / (16 * p.rt);
+    p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+    p.tiles = (rows + p.rows - 1) / p.rows;
     p.heads = lists ? Hq : H;
-    p.units = (long)B * p.heads * (lists ? (Lq + block - 1) / block : 1) * p.tiles;
-    // parts of a walk: until there are four work-groups per compute unit, each
-    // with four steps per wave at least
-    const long want = (1024 + p.units - 1) / p.units;
-    const long most = std::max(1L, ((long)max_len + kStep - 1) / kStep / 16);
-    p.C = (int)std::max(1L, std::min(want, most));
+    p.units = B * p.heads * (lists ? (Lq + block - 1) / block : 1) * p.tiles;
+    if (p.rows >= 128) {
+        // Work-groups run in rounds, one of 256 rows or two of 128 per compute
+        // unit: the number of parts whose rounds end first.  A part costs a
+        // start of about four units, and its partial results are written and
+        // read (in the time of a unit, about 2 us, 9 MB move).  The length of
+        // lists is not known here: they are taken to keep a quarter.
+        const long slots = p.rows == 128 ? 512 : 256;
+        const double walk = std::max(1.0, (lists ? 0.25 : 1.0) * max_len / kUnit);
+        double best = 0.0;
+        p.C = 1;
+        for (int c = 1; c <= 32 && (c == 1 || walk / c >= 8.0); ++c) {
+            const double rounds = (double)(((long)p.units * c + slots - 1) / slots);
+            const double join = c == 1 ? 0.0 : 2.0 + 8.0 * p.units * c * p.rows * d / 9e6;
+            const double cost = rounds * (walk / c + 4.0) + join;
+            if (c == 1 || cost < best) {
+                best = cost;
+                p.C = c;
+            }
+        }
+        return p;
+    }
+    // until there are four work-groups per compute unit, each with four steps
+    // per wave at least
+    const int want = (1024 + p.units - 1) / p.units;
+    const int most = std::max(1, (max_len + kStep - 1) / kStep / 16);
+    p.C = std::max(1, std::min(want, most));
     return p;
 }
 size_t part_bytes(const Plan& p, int d) {
-    return p.C == 1 ? 0 : (size_t)p.units * p.C * 16 * p.rt * (d + 1) * sizeof(float);
+    return p.C == 1 ? 0 : (size_t)p.units * p.C * p.rows * (d + 1) * sizeof(float);
 }
 
-template <int D, int FMT, int RT, bool LISTS>
+template <int D, int FMT, int ROWS, bool LISTS>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
-    const long total = a.units * a.C;
-    const unsigned grid = (unsigned)((total + kXcds - 1) / kXcds * kXcds);
-    hipLaunchKernelGGL((rows_kernel<D, FMT, RT, LISTS>), dim3(grid), dim3(256), 0, s, a);
+    const dim3 grid((unsigned)((a.units * a.C + kXcds - 1) / kXcds * kXcds));
+    if constexpr (ROWS >= 128)
+        hipLaunchKernelGGL((tile_kernel<D, FMT, LISTS, ROWS / 32>), grid, dim3(2 * ROWS), 0, s, a);
+    else
+        hipLaunchKernelGGL((rows_kernel<D, FMT, ROWS / 16, LISTS>), grid, dim3(256), 0, s, a);
     if (a.C > 1) {
         constexpr int RPG = 256 / (D / 4);
-        const long rows = a.units * 16 * RT;
-        hipLaunchKernelGGL((join_kernel<D, 16 * RT, LISTS>), dim3((unsigned)((rows + RPG - 1) / RPG)), dim3(256), 0, s,
-                           a);
+        hipLaunchKernelGGL((join_kernel<D, ROWS, LISTS>), dim3((unsigned)((a.units * ROWS + RPG - 1) / RPG)), dim3(256),
+                           0, s, a);
     }
     return hipGetLastError();
 }
@@ -424,25 +891,27 @@ hipError_t launch(const AttnArgs& a, hipStream_t s) {
 }  // namespace
 
 size_t cache_attn_ws_bytes(int B, int H, int d, int block, int Hq, int Lq, int max_len) {
-    return std::max(part_bytes(plan_of(B, H, block, Hq, Lq, max_len, false), d),
-                    part_bytes(plan_of(B, H, block, Hq, Lq, max_len, true), d));
+    return std::max(part_bytes(plan_of(B, H, d, block, Hq, Lq, max_len, false), d),
+                    part_bytes(plan_of(B, H, d, block, Hq, Lq, max_len, true), d));
 }
 
 hipError_t launch_cache_attn(const CacheView& c, const uint16_t* q, int Hq, int Lq, int max_len,
                              const int32_t* kv_len, const int32_t* kv_idx, const int32_t* kv_cnt, float scale,
                              uint16_t* o, float* lse, void* ws, hipStream_t s) {
     const bool lists = kv_idx != nullptr;
-    const Plan p = plan_of(c.B, c.H, c.block, Hq, Lq, max_len, lists);
+    const Plan p = plan_of(c.B, c.H, c.d, c.block, Hq, Lq, max_len, lists);
     AttnArgs a{q, c.k, c.v, c.ks, c.vs, kv_len, kv_idx, kv_cnt, o, lse, static_cast<float*>(ws),
                c.B, Hq, c.H, Lq, c.cap, c.n, max_len, (max_len + c.block - 1) / c.block,
-               (Lq + c.block - 1) / c.block, c.block, p.tiles, p.heads, p.C, p.units, scale * kLog2e};
+               (Lq + c.block - 1) / c.block, c.block, c.block == 128 ? 7 : 6, Hq / c.H, p.tiles, p.heads, p.C, p.units, scale * kLog2e};
     hipError_t e = hipErrorInvalidValue;
     auto with_rt = [&](auto d, auto fmt, auto ls) {
         constexpr int D = decltype(d)::value, FMT = decltype(fmt)::value;
         constexpr bool LISTS = decltype(ls)::value;
-        if (p.rt == 1) e = launch<D, FMT, 1, LISTS>(a, s);
-        else if (p.rt == 2) e = launch<D, FMT, 2, LISTS>(a, s);
-        else e = launch<D, FMT, 4, LISTS>(a, s);
+        if (p.rows == 16) e = launch<D, FMT, 16, LISTS>(a, s);
+        else if (p.rows == 32) e = launch<D, FMT, 32, LISTS>(a, s);
+        else if (p.rows == 64) e = launch<D, FMT, 64, LISTS>(a, s);
+        else if (p.rows == 128) e = launch<D, FMT, 128, LISTS>(a, s);
+        else if constexpr (!LISTS) e = launch<D, FMT, 256, LISTS>(a, s);
     };
     auto with_fmt = [&](auto d, auto fmt) {
         if (lists) with_rt(d, fmt, std::true_type{});
