@@ -132,6 +132,10 @@ for _name, (_res, _args) in _SIGS.items():
 EXPORTED = tuple(_SIGS)
 
 
+# the current stream's address without a stream object (0.1 us instead of 2.7)
+_current_raw_stream = getattr(getattr(torch, "_C", None), "_cuda_getCurrentRawStream", None)
+
+
 def _status_name(st: int) -> str:
     return _lib.mod_status_string(st).decode()
 
@@ -161,7 +165,8 @@ def _ptr(x, what: str, dtype=None):
 def _stream(stream):
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
-    import torch
+    if _current_raw_stream is not None:
+        return _current_raw_stream(torch.cuda.current_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -272,18 +277,30 @@ def mod_block_sparse_attn_fwd_noalloc(shape: mod_shape, q, k, v, kv_idx, kv_cnt,
 
 # ---------------------------------------------------------------- the cached layer
 
-def _here(x, what: str):
-    """The library launches on the current device: a tensor of another one is refused."""
-    if hasattr(x, "data_ptr") and x.is_cuda and x.device.index != torch.cuda.current_device():
+def _device(x, what: str):
+    """The library launches on the current device: any other tensor is refused."""
+    d = x.get_device()
+    if d < 0:
+        raise ValueError(f"{what} must be a device tensor")
+    if d != torch.cuda.current_device():
         raise ValueError(f"{what} is on {x.device}, but the current device is cuda:{torch.cuda.current_device()}")
 
 
-def _ints(x, B: int, what: str):
-    """[B] int32 on the device, or None."""
-    _here(x, what)
-    if hasattr(x, "shape") and tuple(x.shape) != (B,):
-        raise ValueError(f"{what} must have shape ({B},), got {tuple(x.shape)}")
-    return _ptr(x, what, "torch.int32")
+def _array(x, dims, dtype, what: str):
+    """Address of a contiguous device tensor of that shape (None: any) and
+    type, an int, or None."""
+    if x is None or isinstance(x, int):
+        return x
+    if not hasattr(x, "data_ptr"):
+        raise TypeError(f"{what}: unsupported argument type {type(x)}")
+    if dims is not None and x.shape != dims:
+        raise ValueError(f"{what} must have shape {tuple(dims)}, got {tuple(x.shape)}")
+    if dtype is not None and x.dtype is not dtype:
+        raise ValueError(f"{what} must be {dtype}, got {x.dtype}")
+    if not x.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    _device(x, what)
+    return x.data_ptr()
 
 
 def _strided(x, dims, what: str):
@@ -293,18 +310,17 @@ def _strided(x, dims, what: str):
         return x, None
     if not hasattr(x, "data_ptr"):
         raise TypeError(f"{what}: unsupported argument type {type(x)}")
-    if tuple(x.shape) != tuple(dims):
+    if x.shape != dims:
         raise ValueError(f"{what} must have shape {tuple(dims)}, got {tuple(x.shape)}")
-    if str(x.dtype) != "torch.bfloat16":
+    if x.dtype is not torch.bfloat16:
         raise ValueError(f"{what} must be torch.bfloat16, got {x.dtype}")
-    if not x.is_cuda:
-        raise ValueError(f"{what} must be a device tensor")
-    if x.stride(3) != 1:
+    b, h, t, c = x.stride()
+    if c != 1:
         raise ValueError(f"{what} must have contiguous channels")
-    _here(x, what)
+    _device(x, what)
     # the stride of an axis of one entry is of no account
-    st = [x.stride(i) if x.shape[i] > 1 else 0 for i in range(3)]
-    return x.data_ptr(), ctypes.byref(mod_strides(*st))
+    return x.data_ptr(), ctypes.byref(mod_strides(b if dims[0] > 1 else 0, h if dims[1] > 1 else 0,
+                                                  t if dims[2] > 1 else 0))
 
 
 def make_rope_params(d, dims, grid, theta=10000.0, pairing="adjacent") -> mod_rope_params:
@@ -324,10 +340,9 @@ def make_cache(k, v, k_scale, v_scale) -> mod_cache:
     for x, what in ((k, "k"), (v, "v")):
         if hasattr(x, "element_size") and x.element_size() != 1:
             raise ValueError(f"{what} must have one byte per code, got {x.dtype}")
-    for x, what in ((k, "k"), (v, "v"), (k_scale, "k_scale"), (v_scale, "v_scale")):
-        _here(x, what)
-    return mod_cache(_ptr(k, "k"), _ptr(v, "v"), _ptr(k_scale, "k_scale", "torch.float32"),
-                     _ptr(v_scale, "v_scale", "torch.float32"))
+    return mod_cache(_array(k, None, None, "k"), _array(v, None, None, "v"),
+                     _array(k_scale, None, torch.float32, "k_scale"),
+                     _array(v_scale, None, torch.float32, "v_scale"))
 
 
 def mod_rope_create(params: mod_rope_params) -> int:
@@ -345,8 +360,8 @@ def _rope_call(name, rope, shape, x, y, first, starts, stream):
     src, dst = ("x", "y") if name == "mod_rope_fwd" else ("dy", "dx")
     xp, xs = _strided(x, dims, src)
     yp, ys = _strided(y, dims, dst)
-    _check(getattr(_lib, name)(rope, ctypes.byref(shape), xp, xs, yp, ys, first, _ints(starts, shape.B, "starts"),
-                               _stream(stream)), name)
+    _check(getattr(_lib, name)(rope, ctypes.byref(shape), xp, xs, yp, ys, first,
+                               _array(starts, (shape.B,), torch.int32, "starts"), _stream(stream)), name)
 
 
 def mod_rope_fwd(rope, shape: mod_shape, x, y, first: int = 0, starts=None, stream=None) -> None:
@@ -371,8 +386,8 @@ def _store_call(name, shape, cache, k, v, first, starts, counts, L, stream):
     kp, ks = _strided(k, dims, "k")
     vp, vs = _strided(v, dims, "v")
     _check(getattr(_lib, name)(ctypes.byref(shape), ctypes.byref(cache), kp, ks, vp, vs, L, first,
-                               _ints(starts, shape.B, "starts"), _ints(counts, shape.B, "counts"),
-                               _stream(stream)), name)
+                               _array(starts, (shape.B,), torch.int32, "starts"),
+                               _array(counts, (shape.B,), torch.int32, "counts"), _stream(stream)), name)
 
 
 def mod_cache_write(shape: mod_cache_shape, cache: mod_cache, k, v, first: int = 0, starts=None, counts=None, L=None,
@@ -403,13 +418,10 @@ def mod_cache_attn_fwd(shape: mod_cache_shape, cache: mod_cache, q, max_len: int
             raise ValueError(f"q must have shape ({shape.B}, Hq, Lq, {shape.d}), got {tuple(q.shape)}")
         Hq, Lq = q.shape[1], q.shape[2]
     n, nq = -(-max_len // shape.block), -(-Lq // shape.block)
-    for x, what, dims in ((o, "o", (shape.B, Hq, Lq, shape.d)), (lse, "lse", (shape.B, Hq, Lq)),
-                          (kv_idx, "kv_idx", (shape.B, Hq, nq, n)), (kv_cnt, "kv_cnt", (shape.B, Hq, nq))):
-        if hasattr(x, "shape") and tuple(x.shape) != dims:
-            raise ValueError(f"{what} must have shape {dims}, got {tuple(x.shape)}")
-    for x, what in ((q, "q"), (o, "o"), (lse, "lse"), (kv_idx, "kv_idx"), (kv_cnt, "kv_cnt"),
-                    (workspace, "workspace")):
-        _here(x, what)
+    B, bf16, i32 = shape.B, torch.bfloat16, torch.int32
+    args = (_array(q, None, bf16, "q"), Hq, Lq, max_len, _array(kv_len, (B,), i32, "kv_len"),
+            _array(kv_idx, (B, Hq, nq, n), i32, "kv_idx"), _array(kv_cnt, (B, Hq, nq), i32, "kv_cnt"), float(scale),
+            _array(o, (B, Hq, Lq, shape.d), bf16, "o"), _array(lse, (B, Hq, Lq), torch.float32, "lse"))
     st = _stream(stream)
     if workspace is None and hasattr(q, "device"):
         ws_bytes = mod_cache_attn_workspace_bytes(shape, Hq, Lq, max_len)
@@ -417,11 +429,8 @@ def mod_cache_attn_fwd(shape: mod_cache_shape, cache: mod_cache, q, max_len: int
             workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
             if st != torch.cuda.current_stream().cuda_stream:   # its memory waits for that stream's use of it
                 workspace.record_stream(torch.cuda.ExternalStream(st))
-    _check(_lib.mod_cache_attn_fwd(
-        ctypes.byref(shape), ctypes.byref(cache), _ptr(q, "q", "torch.bfloat16"), Hq, Lq, max_len,
-        _ints(kv_len, shape.B, "kv_len"), _ptr(kv_idx, "kv_idx", "torch.int32"),
-        _ptr(kv_cnt, "kv_cnt", "torch.int32"), float(scale), _ptr(o, "o", "torch.bfloat16"),
-        _ptr(lse, "lse", "torch.float32"), _ptr(workspace, "workspace"), ws_bytes, st), "mod_cache_attn_fwd")
+    _check(_lib.mod_cache_attn_fwd(ctypes.byref(shape), ctypes.byref(cache), *args,
+                                   _array(workspace, None, None, "workspace"), ws_bytes, st), "mod_cache_attn_fwd")
 
 
 def _dbl(n):

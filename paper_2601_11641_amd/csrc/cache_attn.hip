@@ -45,6 +45,19 @@ constexpr int kXcds = 8;
 constexpr int kStep = 32;          // tokens of a wave's step
 constexpr float kSumLimit = 256.0f; // bound on a lane's probability sum per unit while its maximum is kept
 
+template <class F, int... I>
+__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+    static_for_impl(f, std::make_integer_sequence<int, N>{});
+}
+
+// Waves of a work-group of rows_kernel, by its row tiles of 16.
+template <int RT>
+constexpr int kRowWaves = RT == 4 ? 4 : 8;
+
 struct AttnArgs {
     const uint16_t* q;
     const uint8_t *k, *v;
@@ -99,10 +112,13 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, r);
 }
 
-// max / sum over the four lanes that hold a query row's tokens (16 apart)
+// max / sum over the four lanes that hold a query row's tokens (16 apart): a
+// swap with x in both operands leaves both lanes' values in its results
 __device__ __forceinline__ float max4(float x) {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 __device__ __forceinline__ float sum4(float x) {
     x += __shfl_xor(x, 16);
@@ -141,14 +157,14 @@ __device__ __forceinline__ Rows rows_of(const AttnArgs& a, int u) {
 }
 
 template <int D, int FMT, int RT, bool LISTS>
-__global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) {
-    constexpr int ROWS = 16 * RT;
+__global__ __launch_bounds__(64 * kRowWaves<RT>, 1) void rows_kernel(AttnArgs a) {
+    constexpr int ROWS = 16 * RT, WAVES = kRowWaves<RT>;
     constexpr int KC = D / 64;          // 16-byte chunks of a token's K per lane
     constexpr int VF = D / 16;          // channels of V per lane, 16-channel tiles of O^T
     constexpr int VW = VF / 4;          // dwords of V per token and lane
     constexpr int LDO = D + 4;
-    __shared__ float obuf[4][16][LDO];
-    __shared__ float mbuf[4][ROWS], lbuf[4][ROWS];
+    __shared__ float obuf[WAVES][16][LDO];
+    __shared__ float mbuf[WAVES][ROWS], lbuf[WAVES][ROWS];
 
     const int total = a.units * a.C;
     // consecutive work-groups go to the dies in turn: a die takes one stretch of
@@ -167,8 +183,8 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int len = clamp_len(a, r.b);
     const size_t hk = (size_t)r.b * a.H + r.kv;
-    const uint8_t* kp = a.k + hk * a.cap * D + 16 * g;
-    const uint8_t* vp = a.v + hk * a.cap * D + VF * l16;
+    const uint8_t* kp = a.k + hk * a.cap * D;
+    const uint8_t* vp = a.v + hk * a.cap * D;
     const float* ksp = a.ks + hk * a.ncap;
     const float* vsp = a.vs + hk * a.ncap;
     const int ps = a.shift - 5;         // steps per block: 1 << ps
@@ -180,6 +196,52 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
         steps = min(max(a.cnt[lrow], 0), a.n) << ps;
     }
     const int s0 = (int)((long)steps * part / a.C), s1 = (int)((long)steps * (part + 1) / a.C);
+
+    // A step's codes and scales; t0: its first token, -1 where there is none.
+    struct Step {
+        uint4 k[2][KC];
+        uint32_t v[8][VW];
+        float ks, vs;
+        int t0;
+    };
+    auto entry_of = [&](int s) __attribute__((always_inline)) { return LISTS && s < s1 ? list[s >> ps] : 0; };
+    auto load = [&](Step& x, int s, int j) __attribute__((always_inline)) {
+        int t0 = s * kStep;
+        if (LISTS) {
+            j = __builtin_amdgcn_readfirstlane(j);
+            t0 = j * a.block + (s & ((1 << ps) - 1)) * kStep;
+            if (j < 0 || j >= a.n || t0 >= len) t0 = -1;
+        }
+        if (s >= s1) t0 = -1;
+        x.t0 = t0;
+        if (t0 < 0) return;
+        const int last = len - 1 - t0;   // tokens past the end: masked
+        const uint8_t* kb = kp + (size_t)t0 * D;
+        const uint8_t* vb = vp + (size_t)t0 * D;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < KC; ++c)
+                x.k[t][c] = *reinterpret_cast<const uint4*>(kb + (uint32_t)(min(16 * t + l16, last) * D + 64 * c + 16 * g));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint8_t* p = vb + (uint32_t)(min(16 * (e / 4) + 4 * g + e % 4, last) * D + VF * l16);
+            if constexpr (VW == 2) {
+                const uint2 y = *reinterpret_cast<const uint2*>(p);
+                x.v[e][0] = y.x;
+                x.v[e][1] = y.y;
+            } else {
+                x.v[e][0] = *reinterpret_cast<const uint32_t*>(p);
+            }
+        }
+        x.ks = ksp[t0 >> a.shift];
+        x.vs = vsp[t0 >> a.shift];
+    };
+    // two steps are under way: the codes of the next arrive while one is computed
+    Step even, odd;
+    int s = s0 + wave;
+    load(even, s, entry_of(s));
+    int jn = entry_of(s + WAVES);
 
     // Q as the second operand: row l16 of tile rt, the channels that a lane of
     // group g loads of K
@@ -195,7 +257,6 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
             qf[rt][c] = __builtin_bit_cast(bf16x8, x);
         }
     }
-
     f32x4 acc[RT][VF];
     float m[RT], l[RT];
 #pragma unroll
@@ -206,50 +267,16 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
         for (int f = 0; f < VF; ++f) acc[rt][f] = f32x4{0, 0, 0, 0};
     }
 
-    // first token of step s, or -1 where there is none
-    auto token_of = [&](int s) {
-        if (!LISTS) return s * kStep;
-        const int j = list[s >> ps];
-        const int t = j * a.block + (s & ((1 << ps) - 1)) * kStep;
-        return (j < 0 || j >= a.n || t >= len) ? -1 : t;
-    };
-    uint4 kw[2][KC];
-    uint32_t vw[8][VW];
-    float ksc = 0.0f, vsc = 0.0f;
-    auto load = [&](int t0) {
-        const int last = len - 1;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const size_t row = (size_t)min(t0 + 16 * t + l16, last) * D;
-#pragma unroll
-            for (int c = 0; c < KC; ++c) kw[t][c] = *reinterpret_cast<const uint4*>(kp + row + 64 * c);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const size_t row = (size_t)min(t0 + 16 * (e / 4) + 4 * g + e % 4, last) * D;
-            if constexpr (VW == 2) {
-                const uint2 x = *reinterpret_cast<const uint2*>(vp + row);
-                vw[e][0] = x.x;
-                vw[e][1] = x.y;
-            } else {
-                vw[e][0] = *reinterpret_cast<const uint32_t*>(vp + row);
-            }
-        }
-        ksc = ksp[t0 >> a.shift];
-        vsc = vsp[t0 >> a.shift];
-    };
-
-    for (int s = s0 + wave; s < s1; s += 4) {
-        const int t0 = __builtin_amdgcn_readfirstlane(token_of(s));
-        if (t0 < 0) continue;
-        load(t0);
-        const float sc = ksc * a.c2;
+    auto compute = [&](const Step& y) __attribute__((always_inline)) {
+        const int t0 = __builtin_amdgcn_readfirstlane(y.t0);
+        if (t0 < 0) return;
+        const float sc = y.ks * a.c2;
         f32x4 st[RT][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int c = 0; c < 2 * KC; ++c) {
-                const uint4 x = kw[t][c / 2];
+                const uint4 x = y.k[t][c / 2];
                 const bf16x8 kf = c % 2 == 0 ? operand8<FMT>(x.x, x.y) : operand8<FMT>(x.z, x.w);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
@@ -261,11 +288,14 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
         for (int rt = 0; rt < RT; ++rt) {
             float x[8], mx = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[e] = st[rt][e / 4][e % 4] * sc;
-                if (t0 + 16 * (e / 4) + 4 * g + e % 4 >= len) x[e] = -INFINITY;
-                mx = fmaxf(mx, x[e]);
+            for (int e = 0; e < 8; ++e) x[e] = st[rt][e / 4][e % 4] * sc;
+            if (t0 + kStep > len) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (t0 + 16 * (e / 4) + 4 * g + e % 4 >= len) x[e] = -INFINITY;
             }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) mx = fmaxf(mx, x[e]);
             const float mn = fmaxf(m[rt], max4(mx));
             if (__any(mn > m[rt])) {
                 const float alpha = mn > m[rt] ? __builtin_amdgcn_exp2f(m[rt] - mn) : 1.0f;
@@ -279,31 +309,30 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
             for (int e = 0; e < 8; ++e) {
                 const float p = __builtin_amdgcn_exp2f(x[e] - mb);
                 l[rt] += p;
-                pf[rt][e] = static_cast<__bf16>(p * vsc);
+                pf[rt][e] = static_cast<__bf16>(p * y.vs);
             }
         }
-        auto product = [&](auto f_tag) __attribute__((always_inline)) {
+        static_for<VF>([&](auto f_tag) __attribute__((always_inline)) {
             constexpr int F = decltype(f_tag)::value, W = F / 4, BY = F % 4;
-            const u32x4 x = {column_pair<FMT, BY>(vw[0][W], vw[1][W]), column_pair<FMT, BY>(vw[2][W], vw[3][W]),
-                             column_pair<FMT, BY>(vw[4][W], vw[5][W]), column_pair<FMT, BY>(vw[6][W], vw[7][W])};
+            const u32x4 x = {column_pair<FMT, BY>(y.v[0][W], y.v[1][W]), column_pair<FMT, BY>(y.v[2][W], y.v[3][W]),
+                             column_pair<FMT, BY>(y.v[4][W], y.v[5][W]), column_pair<FMT, BY>(y.v[6][W], y.v[7][W])};
             const bf16x8 vf = __builtin_bit_cast(bf16x8, x);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
                 acc[rt][F] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rt], acc[rt][F], 0, 0, 0);
-        };
-        product(std::integral_constant<int, 0>{});
-        product(std::integral_constant<int, 1>{});
-        product(std::integral_constant<int, 2>{});
-        product(std::integral_constant<int, 3>{});
-        if constexpr (VF == 8) {
-            product(std::integral_constant<int, 4>{});
-            product(std::integral_constant<int, 5>{});
-            product(std::integral_constant<int, 6>{});
-            product(std::integral_constant<int, 7>{});
-        }
+        });
+    };
+    while (s < s1) {
+        load(odd, s + WAVES, jn);
+        jn = entry_of(s + 2 * WAVES);
+        compute(even);
+        s += 2 * WAVES;
+        load(even, s, jn);
+        jn = entry_of(s + WAVES);
+        compute(odd);
     }
 
-    // join the four waves
+    // join the waves
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         l[rt] = sum4(l[rt]);
@@ -315,8 +344,9 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
     __syncthreads();
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        const int row = 16 * rt + l16;
-        float top = fmaxf(fmaxf(mbuf[0][row], mbuf[1][row]), fmaxf(mbuf[2][row], mbuf[3][row]));
+        float top = mbuf[0][16 * rt + l16];
+#pragma unroll
+        for (int wv = 1; wv < WAVES; ++wv) top = fmaxf(top, mbuf[wv][16 * rt + l16]);
         const float mine = m[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[rt] - top);
 #pragma unroll
         for (int rr = 0; rr < 4; ++rr)
@@ -326,33 +356,35 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
                     make_float4(acc[rt][f][rr] * mine, acc[rt][f + 1][rr] * mine, acc[rt][f + 2][rr] * mine,
                                 acc[rt][f + 3][rr] * mine);
         __syncthreads();
-        constexpr int W = D / 16;       // channels per thread
-        const int orow = tid / 16, ch = tid % 16 * W, tr = 16 * rt + orow;
-        const float tt = fmaxf(fmaxf(mbuf[0][tr], mbuf[1][tr]), fmaxf(mbuf[2][tr], mbuf[3][tr]));
-        float sum = 0.0f;
+        constexpr int W = D / (4 * WAVES);   // channels per thread
+        const int orow = tid / (4 * WAVES), ch = tid % (4 * WAVES) * W, tr = 16 * rt + orow;
+        float tt = mbuf[0][tr];
 #pragma unroll
-        for (int wv = 0; wv < 4; ++wv)
+        for (int wv = 1; wv < WAVES; ++wv) tt = fmaxf(tt, mbuf[wv][tr]);
+        float sum = 0.0f, out[W];
+#pragma unroll
+        for (int e = 0; e < W; ++e) out[e] = 0.0f;
+#pragma unroll
+        for (int wv = 0; wv < WAVES; ++wv) {
             if (lbuf[wv][tr] != 0.0f)   // 0: that wave kept no token (its maximum may be -inf)
                 sum += lbuf[wv][tr] * __builtin_amdgcn_exp2f(mbuf[wv][tr] - tt);
-        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        float out[W];
 #pragma unroll
-        for (int e = 0; e < W; ++e)
-            out[e] = (obuf[0][orow][ch + e] + obuf[1][orow][ch + e] + obuf[2][orow][ch + e] + obuf[3][orow][ch + e]) * inv;
+            for (int e = 0; e < W; ++e) out[e] += obuf[wv][orow][ch + e];
+        }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
         const float lse2 = sum == 0.0f ? -INFINITY : tt + __builtin_amdgcn_logf(sum);   // log2
-        if (a.C > 1) {
+        if (tr >= r.count) {
+        } else if (a.C > 1) {
             const long slot = ((long)unit * a.C + part) * ROWS + tr;
             float* po = a.part + slot * D + ch;
 #pragma unroll
-            for (int e = 0; e < W; e += 4)
-                *reinterpret_cast<float4*>(po + e) = make_float4(out[e], out[e + 1], out[e + 2], out[e + 3]);
-            if (tid % 16 == 0) (a.part + (long)a.units * a.C * ROWS * D)[slot] = lse2;
-        } else if (tr < r.count) {
+            for (int e = 0; e < W; ++e) po[e] = out[e] * inv;
+            if (tid % (4 * WAVES) == 0) (a.part + (long)a.units * a.C * ROWS * D)[slot] = lse2;
+        } else {
             uint32_t* po = reinterpret_cast<uint32_t*>(a.o + (r.row0 + tr) * D + ch);
 #pragma unroll
-            for (int e = 0; e < W; e += 2)
-                po[e / 2] = pack_bf16(out[e], out[e + 1]);
-            if (a.lse && tid % 16 == 0) a.lse[r.row0 + tr] = lse2 * kLn2;
+            for (int e = 0; e < W; e += 2) po[e / 2] = pack_bf16(out[e] * inv, out[e + 1] * inv);
+            if (a.lse && tid % (4 * WAVES) == 0) a.lse[r.row0 + tr] = lse2 * kLn2;
         }
         __syncthreads();
     }
@@ -375,15 +407,6 @@ __global__ __launch_bounds__(256, RT == 4 ? 1 : 2) void rows_kernel(AttnArgs a) 
 // K and V tiles are double-buffered, V one unit behind K: one barrier a unit.
 // ---------------------------------------------------------------------------
 constexpr int kUnit = 64;
-
-template <class F, int... I>
-__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, I...>) {
-    (f(std::integral_constant<int, I>{}), ...);
-}
-template <int N, class F>
-__device__ __forceinline__ void static_for(F&& f) {
-    static_for_impl(f, std::make_integer_sequence<int, N>{});
-}
 
 // A value that all lanes share, in a scalar register.
 __device__ __forceinline__ float uniform(float x) {
@@ -798,29 +821,72 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
     }
 }
 
-// Joins the parts of every row in their order.  D/4 lanes per row.
-template <int D, int ROWS, bool LISTS>
+// Joins the parts of every row in a fixed order.  D/4 lanes per row and slice of
+// the parts; SLICES slices (8 where a row has many parts) take every eighth
+// part each, and are joined through LDS.
+template <int D, int ROWS, bool LISTS, int SLICES>
 __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
-    constexpr int LPR = D / 4, RPG = 256 / LPR;
-    const int tid = threadIdx.x;
-    const int row = (int)blockIdx.x * RPG + tid / LPR, unit = row / ROWS;
-    if (unit >= a.units) return;
+    constexpr int LPR = D / 4, RPG = 256 / (LPR * SLICES);
+    __shared__ float4 obuf[SLICES > 1 ? 256 : 1];
+    __shared__ float mbuf[SLICES > 1 ? 256 : 1], lbuf[SLICES > 1 ? 256 : 1];
+    const int tid = threadIdx.x, slice = tid / LPR % SLICES;
+    const int row = (int)blockIdx.x * RPG + tid / (LPR * SLICES), unit = row / ROWS;
     const int tr = row % ROWS, ch = tid % LPR * 4;
-    const Rows r = rows_of<ROWS, LISTS>(a, unit);
-    if (tr >= r.count) return;
+    Rows r{};
+    if (unit < a.units) r = rows_of<ROWS, LISTS>(a, unit);
+    const bool live = unit < a.units && tr < r.count;
     const float* lse2 = a.part + (long)a.units * a.C * ROWS * D + (long)unit * a.C * ROWS + tr;
     const float* po = a.part + ((long)unit * a.C * ROWS + tr) * D + ch;
-    float top = -INFINITY;
-    for (int c = 0; c < a.C; ++c) top = fmaxf(top, lse2[(long)c * ROWS]);
-    float sum = 0.0f;
+    float top = -INFINITY, sum = 0.0f;
     f32x4 o = {0, 0, 0, 0};
-    for (int c = 0; c < a.C; ++c) {
-        const float x = lse2[(long)c * ROWS];
-        if (x == -INFINITY) continue;      // that part kept no token
-        const float w = __builtin_amdgcn_exp2f(x - top);
-        sum += w;
-        o += w * *reinterpret_cast<const f32x4*>(po + (long)c * ROWS * D);
+    if (live) {
+        // eight parts at once, their loads together (a part past the last: the last,
+        // without weight)
+        for (int c0 = slice; c0 < a.C; c0 += 8 * SLICES) {
+            float x[8];
+            f32x4 y[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const long c = min(c0 + i * SLICES, a.C - 1);
+                x[i] = lse2[c * ROWS];
+                y[i] = *reinterpret_cast<const f32x4*>(po + c * ROWS * D);
+            }
+            float mn = top;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (c0 + i * SLICES >= a.C) x[i] = -INFINITY;
+                mn = fmaxf(mn, x[i]);
+            }
+            const float keep = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - mn);
+            top = mn;
+            sum *= keep;
+            o *= keep;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float w = x[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x[i] - mn);   // no token: O is 0
+                sum += w;
+                o += y[i] * w;
+            }
+        }
     }
+    if constexpr (SLICES > 1) {
+        obuf[tid] = make_float4(o[0], o[1], o[2], o[3]);
+        mbuf[tid] = top;
+        lbuf[tid] = sum;
+        __syncthreads();
+        if (slice != 0) return;
+        for (int t = 1; t < SLICES; ++t) {
+            const int at = tid + t * LPR;
+            const float x = mbuf[at], mn = fmaxf(top, x);
+            const float keep = top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - mn);
+            const float w = x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(x - mn);
+            const float4 y = obuf[at];
+            top = mn;
+            sum = lbuf[at] != 0.0f ? sum * keep + lbuf[at] * w : sum;
+            if (lbuf[at] != 0.0f) o = o * keep + f32x4{y.x, y.y, y.z, y.w} * w;
+        }
+    }
+    if (!live) return;
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     *reinterpret_cast<uint2*>(a.o + (r.row0 + tr) * D + ch) =
         make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
@@ -835,39 +901,52 @@ struct Plan {
     int tiles, heads, units;
 };
 Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool lists) {
-    Plan p;
     const int rows = lists ? std::min(block, Lq) : (int)std::min<long>((long)(Hq / H) * Lq, 1L << 30);
-    p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
-    p.tiles = (rows + p.rows - 1) / p.rows;
-    p.heads = lists ? Hq : H;
-    p.units = B * p.heads * (lists ? (Lq + block - 1) / block : 1) * p.tiles;
-    if (p.rows >= 128) {
-        // Work-groups run in rounds, one of 256 rows or two of 128 per compute
-        // unit: the number of parts whose rounds end first.  A part costs a
-        // start of about four units, and its partial results are written and
-        // read (in the time of a unit, about 2 us, 9 MB move).  The length of
-        // lists is not known here: they are taken to keep a quarter.
-        const long slots = p.rows == 128 ? 512 : 256;
-        const double walk = std::max(1.0, (lists ? 0.25 : 1.0) * max_len / kUnit);
-        double best = 0.0;
-        p.C = 1;
-        for (int c = 1; c <= 32 && (c == 1 || walk / c >= 8.0); ++c) {
-            const double rounds = (double)(((long)p.units * c + slots - 1) / slots);
-            const double join = c == 1 ? 0.0 : 2.0 + 8.0 * p.units * c * p.rows * d / 9e6;
-            const double cost = rounds * (walk / c + 4.0) + join;
-            if (c == 1 || cost < best) {
-                best = cost;
-                p.C = c;
+    Plan best{};
+    double least = 0.0;
+    // Work-groups run in rounds: the form and the number of parts whose rounds
+    // end first.  A part costs a start, and its partial results are written and
+    // read.  The length of lists is not known here: they are taken to keep a
+    // quarter.
+    auto consider = [&](int tile) {
+        Plan p;
+        p.rows = tile;
+        p.tiles = (rows + tile - 1) / tile;
+        p.heads = lists ? Hq : H;
+        p.units = B * p.heads * (lists ? (Lq + block - 1) / block : 1) * p.tiles;
+        const bool small = tile <= 64;
+        // resident work-groups; tokens of one turn of a work-group (a step of all
+        // its waves, a unit)
+        const int slots = tile == 128 ? 512 : 256;
+        const int turn = small ? kStep * (tile == 64 ? kRowWaves<4> : kRowWaves<1>) : kUnit;
+        const double walk = std::max(1.0, (lists ? 0.25 : 1.0) * max_len / turn);
+        const double exist = (double)std::min(tile, rows);
+        for (int c = 1; c <= 256 && (c == 1 || walk / c >= 1.0); ++c) {
+            p.C = c;
+            const long items = (long)p.units * c;
+            const double rounds = (double)((items + slots - 1) / slots);
+            // microseconds of a turn (the loads' latency, or the share of 5.5 TB/s
+            // that the resident work-groups leave to one; products and softmax), of
+            // a start, and of a join (a launch; its partial results at 4.5 TB/s)
+            const double us = small ? 1.0 + 2.0 * turn * d * std::min<long>(items, slots) / 8.5e6
+                                    : (tile == 128 ? 2.3 : 2.1) * (items <= 256 && tile == 128 ? 0.7 : 1.0);
+            const double start = small ? 3.0 : 8.0;
+            const double join = c == 1 ? 0.0 : 5.0 + 0.02 * c + 8.0 * items * exist * d / 4.5e6;
+            const double cost = rounds * (walk / c * us + start) + join;
+            if (least == 0.0 || cost < least) {
+                least = cost;
+                best = p;
             }
         }
-        return p;
+    };
+    if (rows <= 16) consider(16);
+    else if (rows <= 32) consider(32);
+    else if (rows <= 64 && lists) consider(64);
+    else {
+        consider(128);
+        if (!lists && rows > 128) consider(256);
     }
-    // until there are four work-groups per compute unit, each with four steps
-    // per wave at least
-    const int want = (1024 + p.units - 1) / p.units;
-    const int most = std::max(1, (max_len + kStep - 1) / kStep / 16);
-    p.C = std::max(1, std::min(want, most));
-    return p;
+    return best;
 }
 size_t part_bytes(const Plan& p, int d) {
     return p.C == 1 ? 0 : (size_t)p.units * p.C * p.rows * (d + 1) * sizeof(float);
@@ -879,11 +958,15 @@ hipError_t launch(const AttnArgs& a, hipStream_t s) {
     if constexpr (ROWS >= 128)
         hipLaunchKernelGGL((tile_kernel<D, FMT, LISTS, ROWS / 32>), grid, dim3(2 * ROWS), 0, s, a);
     else
-        hipLaunchKernelGGL((rows_kernel<D, FMT, ROWS / 16, LISTS>), grid, dim3(256), 0, s, a);
+        hipLaunchKernelGGL((rows_kernel<D, FMT, ROWS / 16, LISTS>), grid, dim3(64 * kRowWaves<ROWS / 16>), 0, s, a);
     if (a.C > 1) {
-        constexpr int RPG = 256 / (D / 4);
-        hipLaunchKernelGGL((join_kernel<D, ROWS, LISTS>), dim3((unsigned)((a.units * ROWS + RPG - 1) / RPG)), dim3(256),
-                           0, s, a);
+        auto join = [&](auto slices) {
+            constexpr int SL = decltype(slices)::value, RPG = 256 / (D / 4 * SL);
+            hipLaunchKernelGGL((join_kernel<D, ROWS, LISTS, SL>), dim3((unsigned)((a.units * ROWS + RPG - 1) / RPG)),
+                               dim3(256), 0, s, a);
+        };
+        if (a.C > 8) join(std::integral_constant<int, 8>{});
+        else join(std::integral_constant<int, 1>{});
     }
     return hipGetLastError();
 }
@@ -909,7 +992,9 @@ hipError_t launch_cache_attn(const CacheView& c, const uint16_t* q, int Hq, int 
         constexpr bool LISTS = decltype(ls)::value;
         if (p.rows == 16) e = launch<D, FMT, 16, LISTS>(a, s);
         else if (p.rows == 32) e = launch<D, FMT, 32, LISTS>(a, s);
-        else if (p.rows == 64) e = launch<D, FMT, 64, LISTS>(a, s);
+        else if (p.rows == 64) {
+            if constexpr (LISTS) e = launch<D, FMT, 64, LISTS>(a, s);
+        }
         else if (p.rows == 128) e = launch<D, FMT, 128, LISTS>(a, s);
         else if constexpr (!LISTS) e = launch<D, FMT, 256, LISTS>(a, s);
     };
