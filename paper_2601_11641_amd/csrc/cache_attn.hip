@@ -436,12 +436,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
     constexpr int NP = CPT / PIECE;              // each of a token TPP after the other's
     constexpr int TPR = D / PIECE, TPP = 64 * WAVES / TPR;
     constexpr int PW = PIECE / 4;                // dwords of a piece
-    // With eight waves, which alone fill a compute unit, three buffers: the
-    // barrier lies between the halves, behind the conversion of both tiles, and
-    // no operand read waits for it.  With four, two work-groups share the unit
-    // and cover each other; two buffers each, and the barrier at the unit's end.
-    constexpr int NB = WAVES == 8 ? 3 : 2;
-    __shared__ __align__(1024) char lds[NB * (KTILE + VTILE)];
+    __shared__ __align__(1024) char lds[2 * KTILE + 2 * VTILE];   // K, K, V, V
 
     const int total = a.units * a.C, per = (total + kXcds - 1) / kXcds;
     const int w = (int)(blockIdx.x % kXcds) * per + (int)(blockIdx.x / kXcds);
@@ -490,13 +485,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
     const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)lds;
     const int s16 = lane & 15;
     const uint32_t kad = lds0 + (uint32_t)(l32 * KROW + 16 * h);
-    const uint32_t vad = lds0 + (uint32_t)(NB * KTILE + (4 * h + (s16 >> 2)) * VROW + 32 * (lane >> 4 & 1) + 8 * (s16 & 3));
+    const uint32_t vad = lds0 + (uint32_t)(2 * KTILE + (4 * h + (s16 >> 2)) * VROW + 32 * (lane >> 4 & 1) + 8 * (s16 & 3));
 
     // staging: thread tid brings a piece of a token's codes, one or two 16-byte
     // chunks of its LDS row
     const int scol = tid % TPR, srow = tid / TPR;
     char* const kst = lds + srow * KROW + 2 * PIECE * scol;
-    char* const vst = lds + NB * KTILE + srow * VROW + 2 * PIECE * scol;
+    char* const vst = lds + 2 * KTILE + srow * VROW + 2 * PIECE * scol;
     uint32_t kr[NP][PW], vr[NP][PW];
     auto entry_of = [&](int u) __attribute__((always_inline)) { return LISTS ? list[(u0 + u) >> us] : 0; };
     // first token of unit u, whose list entry is j; -1: nothing to read
@@ -731,38 +726,27 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
     Unit before{}, now{};
     // One unit, its K at kc and the V of the unit before at vp: its scores, the
     // rest of the unit before, and half of its softmax.
-    int kc = 0, vp = (NB - 1) * VTILE;
+    int kc = 0, vp = VTILE;
     auto iterate = [&](int t, auto first_tag) __attribute__((always_inline)) {
         using Rest = std::bool_constant<!decltype(first_tag)::value>;
-        using Mid = std::bool_constant<NB == 3>;             // both tiles are converted in the first half
-        using End = std::bool_constant<NB != 3>;
-        const int kn = kc == (NB - 1) * KTILE ? 0 : kc + KTILE, vc = vp == (NB - 1) * VTILE ? 0 : vp + VTILE;
+        const int kn = KTILE - kc, vc = VTILE - vp;
         const uint32_t ka = kad + kc, va = vad + vp;
         char* const vto = vst + vc;
         float ksn, vsn;
         fetch_scales(tn, ksn, vsn);
-        half(I0{}, ka, va, Yes{}, Rest{}, Rest{}, Yes{}, Mid{}, Yes{}, before, kst + kn, vto, ka + 32 * KROW,
+        half(I0{}, ka, va, Yes{}, Rest{}, Rest{}, Yes{}, No{}, Yes{}, before, kst + kn, vto, ka + 32 * KROW,
              va + 32 * VROW);
-        const bool special = !(vs >= 0x1p-64f && vs <= 0x1p64f);
-        if constexpr (NB == 3) {
-            if (special) stage_scaled(vto, vs);
-            barrier();
-            if (t + 1 < T) load(vcodes, tn, vr);
-        }
         int tnn = -1;
         if (t + 2 < T) {
             tnn = token_of(t + 2, jn);
             load(kcodes, tnn, kr);
             if (t + 3 < T) jn = entry_of(t + 3);
         }
-        half(I1{}, ka + 32 * KROW, va + 32 * VROW, Yes{}, Yes{}, Rest{}, No{}, End{}, Mid{}, now, kst, vto, kad + kn,
-             vad + vc);
-        if constexpr (NB == 2) {
-            if (special) stage_scaled(vto, vs);
-            if (t + 1 < T) load(vcodes, tn, vr);
-            barrier();
-            read_ahead(kad + kn, vad + vc);
-        }
+        half(I1{}, ka + 32 * KROW, va + 32 * VROW, Yes{}, Yes{}, Rest{}, No{}, Yes{}, No{}, now, kst, vto, 0, 0);
+        if (!(vs >= 0x1p-64f && vs <= 0x1p64f)) stage_scaled(vto, vs);
+        if (t + 1 < T) load(vcodes, tn, vr);
+        barrier();
+        read_ahead(kad + kn, vad + vc);
         before = now;
         now = unit_of(tn, ksn, vsn);
         vs = uniform(vsn);
