@@ -111,6 +111,11 @@ def parse():
                     help="the Eq. 2 count pass of a dense step on the Hunyuan 720p layer alone "
                          "(mod_update_stats over full lists with the dense attention's LSE): "
                          "time per update and the rate on its QK^T flops; one JSON line")
+    ap.add_argument("--stream", action="store_true",
+                    help="the streamed Hunyuan 720p layer on an 8-bit cache (E4M3, then INT8): a chunk "
+                         "of three frames rotated, written and attended from against all 33 frames, and "
+                         "the whole layer's attention over predicted lists (mass 0.75) on the cache next "
+                         "to the bf16 one; one JSON line per format")
     ap.add_argument("--trace-summary", nargs=2, metavar=("STATS_CSV", "BENCH_LOG"),
                     help="format a rocprofv3 --kernel-trace --stats CSV of a bench run (and the JSON "
                          "line that run printed) into profiles/hunyuan720p_step_kernel_stats.md and exit")
@@ -556,6 +561,88 @@ def run_share(args):
         }), flush=True)
 
 
+def run_stream(args):
+    """The layer as a streamed video runs it, per cache format: the times of
+    one chunk's stages (three latent frames against the whole video) and of
+    the whole layer's sparse attention on the cache."""
+    import numpy as np
+    import torch
+
+    import paper_2601_11641_amd as M
+    import workloads as W
+
+    cfg = W.CONFIGS["hunyuan"]
+    dev = torch.device("cuda:0")
+    q, k, v = (torch.from_numpy(x.view(np.int16)).view(torch.bfloat16).to(dev) for x in W.generate(cfg))
+    stream = torch.cuda.current_stream()
+    reps = max(args.steps, 5)
+    shape = M.make_shape(cfg.B, cfg.H, cfg.L, cfg.d, cfg.block, cfg.frame_tokens)
+    st = M.Stats(shape, M.make_params(warmup_m=WARMUP_M, delta_t=1))
+    n = st.n
+    kv_idx = torch.empty((cfg.B, cfg.H, n, n), dtype=torch.int32, device=dev)
+    kv_cnt = torch.empty((cfg.B, cfg.H, n), dtype=torch.int32, device=dev)
+    M.mod_collect_stats(st.handle, q, k, WARMUP_M)
+    M.mod_predict_block_mask(st.handle, q, k, WARMUP_M + 1, M.make_budget("mass", mass=0.75), kv_idx, kv_cnt)
+    flops = kept_flops(kv_idx, kv_cnt, cfg.L, cfg.block, cfg.d)
+    out, lse = torch.empty_like(q), torch.empty((cfg.B, cfg.H, cfg.L), device=dev)
+
+    def timed(fn):
+        for _ in range(args.warmup):
+            fn()
+        return _median_ms(fn, reps, stream)
+
+    ws = torch.empty(M.mod_attn_workspace_bytes(shape), dtype=torch.uint8, device=dev)
+    bf16_ms = timed(lambda: M.mod_block_sparse_attn_fwd(shape, q, k, v, kv_idx, kv_cnt, 0.0, out, lse, ws, ws.numel()))
+
+    frames, L = 3, 3 * cfg.frame_tokens
+    first = cfg.L - L
+    chunk = M.make_shape(cfg.B, cfg.H, L, cfg.d, cfg.block, cfg.frame_tokens)
+    rope = M.Rope(M.make_rope_params(cfg.d, (16, 56, 56), (cfg.frames, cfg.hs, cfg.ws), theta=256.0))
+    # a chunk as the projection leaves it: token-major, the three operands side by side
+    qkv = torch.stack([x[:, :, first:].transpose(1, 2) for x in (q, k, v)], 2).contiguous()
+    qc, kc, vc = (qkv[:, :, i].transpose(1, 2) for i in range(3))
+    qr, kr = (torch.empty((cfg.B, cfg.H, L, cfg.d), dtype=torch.bfloat16, device=dev) for _ in range(2))
+    oc = torch.empty_like(qr)
+    for fmt in ("e4m3", "int8"):
+        cs = M.make_cache_shape(cfg.B, cfg.H, cfg.L, cfg.d, cfg.block, fmt)
+        cache = M.Cache(cs, dev)
+        whole_write_ms = timed(lambda: M.mod_cache_write(cs, cache.ref, k, v))
+        cws = torch.empty(max(M.mod_cache_attn_workspace_bytes(cs, cfg.H, n_q, cfg.L) for n_q in (L, cfg.L)) or 1,
+                          dtype=torch.uint8, device=dev)
+        sparse = lambda: M.mod_cache_attn_fwd(cs, cache.ref, q, cfg.L, None, kv_idx, kv_cnt, 0.0, out, lse,  # noqa: E731
+                                              cws, cws.numel())
+        sparse_ms = timed(sparse)
+
+        def rotate():
+            M.mod_rope_fwd(rope.handle, chunk, qc, qr, first)
+            M.mod_rope_fwd(rope.handle, chunk, kc, kr, first)
+        rope_ms = timed(rotate)
+        write_ms = timed(lambda: M.mod_cache_write(cs, cache.ref, kr, vc, first))
+        chunk_ms = timed(lambda: M.mod_cache_attn_fwd(cs, cache.ref, qr, cfg.L, None, None, None, 0.0, oc, None, cws,
+                                                      cws.numel()))
+        token_q, token_o = qr[:, :, :1].contiguous(), torch.empty_like(qr[:, :, :1])
+        token_ms = timed(lambda: M.mod_cache_attn_fwd(cs, cache.ref, token_q, cfg.L, None, None, None, 0.0, token_o,
+                                                      None, cws, cws.numel()))
+        chunk_flops = 4.0 * cfg.d * cfg.B * cfg.H * L * cfg.L
+        print(json.dumps({
+            "workload": f"streamed hunyuan-720p layer: B=1 H={cfg.H} L={cfg.L} d={cfg.d} block={cfg.block}, cache {fmt}, "
+                        f"chunks of {frames} frames ({L} tokens)",
+            "cache_gb": round(2 * cache.k.numel() / 1e9, 3),
+            "rope_qk_ms": round(rope_ms, 4), "write_ms": round(write_ms, 4),
+            "chunk_attn_ms": round(chunk_ms, 3),
+            "chunk_attn_tflops": round(chunk_flops / chunk_ms / 1e9, 1),
+            "token_attn_ms": round(token_ms, 4),
+            "token_attn_gbs": round(2 * cache.k.numel() / token_ms / 1e6, 1),
+            "layer_write_ms": round(whole_write_ms, 3),
+            "layer_sparse_attn_ms": round(sparse_ms, 3),
+            "layer_sparse_attn_tflops": round(flops / sparse_ms / 1e9, 1),
+            "layer_sparse_bf16_ms": round(bf16_ms, 3),
+            "layer_sparse_bf16_tflops": round(flops / bf16_ms / 1e9, 1),
+        }), flush=True)
+    rope.close()
+    st.close()
+
+
 def run_count(args):
     """Eq. 2 statistic of a dense step on the Hunyuan 720p layer: one dense
     attention for the row LSE, then --warmup untimed and --steps timed
@@ -736,6 +823,9 @@ def main():
         return
     if args.share:
         run_share(args)
+        return
+    if args.stream:
+        run_stream(args)
         return
 
     import numpy as np

@@ -310,8 +310,9 @@ typedef struct mod_rope mod_rope;   /* opaque, library-owned */
 
 /* Build the (cos, sin) tables of the axes on the host in fp64 and upload them
  * as fp32 (4 * (frames*dims[0] + height*dims[1] + width*dims[2]) bytes on the
- * current device).  Synchronous.  The handle is not changed by its use: any
- * number of calls and streams of that device may share it. */
+ * current device, which has to be current in its calls too).  Synchronous.
+ * The handle is not changed by its use: any number of calls and streams of
+ * that device may share it. */
 mod_status mod_rope_create(const mod_rope_params* params, mod_rope** out);
 
 /* Release the handle (waits for the device).  NULL is accepted. */

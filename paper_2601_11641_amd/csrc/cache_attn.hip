@@ -72,6 +72,7 @@ struct AttnArgs {
     int tiles;                 // row tiles per head and query block (lists) or key/value head
     int heads;                 // heads that items count: Hq with lists, H without
     int C;                     // parts of a walk
+    int stretch;               // consecutive items of a die
     int units;                 // B * heads * (lists: nq) * tiles
     float c2;                  // scale * log2(e)
 };
@@ -156,6 +157,22 @@ __device__ __forceinline__ Rows rows_of(const AttnArgs& a, int u) {
     return r;
 }
 
+// This work-group's item; false: none.  Items are ordered by head, part of the
+// walk, then the tiles that share it.  Consecutive work-groups go to the dies
+// in turn; a die takes `stretch` consecutive items (an eighth of the tiles of a
+// part, which read the same or nearly the same tokens), then every eighth such
+// stretch: heads and sequences of different lengths spread over all dies.
+template <bool LISTS>
+__device__ __forceinline__ bool item_of(const AttnArgs& a, int& unit, int& part) {
+    const int i = (int)(blockIdx.x / kXcds), x = (int)(blockIdx.x % kXcds);
+    const int w = (i / a.stretch * kXcds + x) * a.stretch + i % a.stretch;
+    const int tiles = (LISTS ? a.nq : 1) * a.tiles;
+    const int hb = w / (tiles * a.C), rest = w % (tiles * a.C);
+    part = rest / tiles;
+    unit = hb * tiles + rest % tiles;
+    return w < a.units * a.C;
+}
+
 template <int D, int FMT, int RT, bool LISTS>
 __global__ __launch_bounds__(64 * kRowWaves<RT>, 1) void rows_kernel(AttnArgs a) {
     constexpr int ROWS = 16 * RT, WAVES = kRowWaves<RT>;
@@ -166,16 +183,8 @@ __global__ __launch_bounds__(64 * kRowWaves<RT>, 1) void rows_kernel(AttnArgs a)
     __shared__ float obuf[WAVES][16][LDO];
     __shared__ float mbuf[WAVES][ROWS], lbuf[WAVES][ROWS];
 
-    const int total = a.units * a.C;
-    // consecutive work-groups go to the dies in turn: a die takes one stretch of
-    // the items, whose neighbours read the same tokens
-    const int per = (total + kXcds - 1) / kXcds;
-    const int w = (int)(blockIdx.x % kXcds) * per + (int)(blockIdx.x / kXcds);
-    if ((int)(blockIdx.x / kXcds) >= per || w >= total) return;
-    // order: head, part of the walk, then the tiles that share it
-    const int tiles = (LISTS ? a.nq : 1) * a.tiles;
-    const int hb = w / (tiles * a.C), rest = w % (tiles * a.C);
-    const int part = rest / tiles, unit = hb * tiles + rest % tiles;
+    int unit, part;
+    if (!item_of<LISTS>(a, unit, part)) return;
     const Rows r = rows_of<ROWS, LISTS>(a, unit);
     if (r.count <= 0) return;           // a tile past a short query block
 
@@ -438,15 +447,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
     constexpr int PW = PIECE / 4;                // dwords of a piece
     __shared__ __align__(1024) char lds[2 * KTILE + 2 * VTILE];   // K, K, V, V
 
-    const int total = a.units * a.C, per = (total + kXcds - 1) / kXcds;
-    const int w = (int)(blockIdx.x % kXcds) * per + (int)(blockIdx.x / kXcds);
-    if ((int)(blockIdx.x / kXcds) >= per || w >= total) return;
+    int unit, part;
+    if (!item_of<LISTS>(a, unit, part)) return;
     const int tid = threadIdx.x, lane = tid & 63;
     const int qw = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, h = lane >> 5;
-    const int tiles = (LISTS ? a.nq : 1) * a.tiles;
-    const int hb = w / (tiles * a.C), rest = w % (tiles * a.C);
-    const int part = rest / tiles, unit = hb * tiles + rest % tiles;
     const Rows r = rows_of<ROWS, LISTS>(a, unit);
     if (r.count <= 0) return;                    // a tile past a short query block
 
@@ -906,8 +911,9 @@ Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool l
         const double walk = std::max(1.0, (lists ? 0.25 : 1.0) * max_len / turn);
         const double exist = (double)std::min(tile, rows);
         for (int c = 1; c <= 256 && (c == 1 || walk / c >= 1.0); ++c) {
-            p.C = c;
             const long items = (long)p.units * c;
+            if (c > 1 && items > (1L << 18)) break;      // (and a launch's work-groups keep to their limit)
+            p.C = c;
             const double rounds = (double)((items + slots - 1) / slots);
             // microseconds of a turn (the loads' latency, or the share of 5.5 TB/s
             // that the resident work-groups leave to one; products and softmax), of
@@ -938,7 +944,8 @@ size_t part_bytes(const Plan& p, int d) {
 
 template <int D, int FMT, int ROWS, bool LISTS>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)((a.units * a.C + kXcds - 1) / kXcds * kXcds));
+    const int round = kXcds * a.stretch;
+    const dim3 grid((unsigned)((a.units * a.C + round - 1) / round * round));
     if constexpr (ROWS >= 128)
         hipLaunchKernelGGL((tile_kernel<D, FMT, LISTS, ROWS / 32>), grid, dim3(2 * ROWS), 0, s, a);
     else
@@ -969,7 +976,8 @@ hipError_t launch_cache_attn(const CacheView& c, const uint16_t* q, int Hq, int 
     const Plan p = plan_of(c.B, c.H, c.d, c.block, Hq, Lq, max_len, lists);
     AttnArgs a{q, c.k, c.v, c.ks, c.vs, kv_len, kv_idx, kv_cnt, o, lse, static_cast<float*>(ws),
                c.B, Hq, c.H, Lq, c.cap, c.n, max_len, (max_len + c.block - 1) / c.block,
-               (Lq + c.block - 1) / c.block, c.block, c.block == 128 ? 7 : 6, Hq / c.H, p.tiles, p.heads, p.C, p.units, scale * kLog2e};
+               (Lq + c.block - 1) / c.block, c.block, c.block == 128 ? 7 : 6, Hq / c.H, p.tiles, p.heads, p.C,
+               ((lists ? (Lq + c.block - 1) / c.block : 1) * p.tiles + kXcds - 1) / kXcds, p.units, scale * kLog2e};
     hipError_t e = hipErrorInvalidValue;
     auto with_rt = [&](auto d, auto fmt, auto ls) {
         constexpr int D = decltype(d)::value, FMT = decltype(fmt)::value;

@@ -12,6 +12,7 @@ using moddit::hip_fail;
 
 struct mod_rope {
     mod_rope_params params{};
+    int device = 0;
     float2* table = nullptr;
     moddit::RopeTable view{};
 };
@@ -20,7 +21,7 @@ namespace {
 
 constexpr int kMaxCapacity = 1 << 24;   // a head's codes stay below 2^31 bytes
 constexpr long kMaxHeads = 1L << 22;    // B * H
-constexpr long kMaxGroups = 1L << 23;   // work-groups of a launch (below 2^32 threads)
+constexpr long kMaxGroups = 1L << 22;   // work-groups of a launch (their threads stay below 2^32)
 
 mod_status check_aligned(const void* p, const char* what) {
     if (reinterpret_cast<uintptr_t>(p) % 16 != 0)
@@ -117,6 +118,10 @@ mod_status rope_call(const mod_rope* rope, const mod_shape* shape, const void* x
     if (shape->text_tokens < 0 || shape->text_tokens > shape->L)
         return fail(MOD_ERR_INVALID_ARG, "text_tokens=%d must be in [0, L]", shape->text_tokens);
     if (first < 0) return fail(MOD_ERR_INVALID_ARG, "first=%d must be >= 0", first);
+    int device = -1;
+    if (hipGetDevice(&device) != hipSuccess || device != rope->device)
+        return fail(MOD_ERR_INVALID_ARG, "the rope belongs to device %d, but the current device is %d", rope->device,
+                    device);
     const long total = (long)p.frames * p.height * p.width;
     if (!starts && (long)first + shape->L - shape->text_tokens > total)
         return fail(MOD_ERR_INVALID_ARG, "%d tokens from position %d exceed the %ld positions of the rope",
@@ -170,6 +175,7 @@ mod_status mod_rope_create(const mod_rope_params* params, mod_rope** out) {
     mod_rope* r = new (std::nothrow) mod_rope();
     if (!r) return fail(MOD_ERR_NOMEM, "host allocation failed");
     r->params = p;
+    (void)hipGetDevice(&r->device);
     try {
         table.reserve((size_t)entries);
         for (int a = 0; a < 3; ++a) {
@@ -286,6 +292,7 @@ mod_status mod_cache_attn_fwd(const mod_cache_shape* shape, const mod_cache* cac
     st = check_aligned(q, "q");
     if (st == MOD_OK) st = check_aligned(o, "o");
     if (st != MOD_OK) return st;
+    if (max_len == 0) kv_idx = kv_cnt = nullptr;      // no blocks, no lists
     if (!kv_idx != !kv_cnt) return fail(MOD_ERR_INVALID_ARG, "kv_idx and kv_cnt must both be given, or neither");
     if (!(scale >= 0.0f) || !std::isfinite(scale))
         return fail(MOD_ERR_INVALID_ARG, "scale must be finite and >= 0");

@@ -342,3 +342,80 @@ def test_layer_of_a_stream_of_frames(M, fmt):
         w, wl, eo, el = R.attention(allq.cpu(), *F.kv, [total], block, d ** -0.5, kept)
         assert torch.all((o.double() - o2.double()).cpu().abs() <= 2 * eo)
         assert torch.all((lse.double() - lse2.double()).cpu().abs() <= 2 * el)
+
+
+@pytest.mark.parametrize("fmt", [R.E4M3, R.INT8])
+@pytest.mark.parametrize("Lq,lists", [(1, False), (150, False), (600, False), (150, True)])
+def test_scales_of_any_size(M, fmt, Lq, lists):
+    """Value scales from 2^-100 to 2^100 (side by side in a walk) and zero, key
+    scales of zero."""
+    d, block, n = 128, 128, 9
+    f = Filled(M, 1, 2, n * block, d, block, fmt, [n * block], seed=8)
+    for t, vals in ((1, [2.0 ** -100, 1.0, 0.0, 2.0 ** 66, 2.0 ** -66, 3.0, 2.0 ** 100, 0.0, 2.0 ** -3]), (0, [None] * 4 + [0.0] * 2)):
+        for j, x in enumerate(vals):
+            if x is not None:
+                f.scales[t][:, :, j] = x
+    f.dev[2].copy_(f.scales[0])
+    f.dev[3].copy_(f.scales[1])
+    f.kv = tuple(R.dequant_by(c, s, fmt, block) for c, s in zip(f.codes, f.scales))
+    q = queries(1, 2, Lq, d, 3)
+    idx = cnt = kept = None
+    if lists:   # the rows of every query block end with another of the scales
+        nq = -(-Lq // block)
+        kept = [[[[j for j in range(n) if j != 6 and (j + h + i) % 3] for i in range(nq)] for h in range(2)]]
+        idx = torch.zeros((1, 2, nq, n), dtype=torch.int32)
+        cnt = torch.zeros((1, 2, nq), dtype=torch.int32)
+        for h in range(2):
+            for i in range(nq):
+                js = kept[0][h][i]
+                idx[0, h, i, :len(js)] = torch.tensor(js, dtype=torch.int32)
+                cnt[0, h, i] = len(js)
+    o, lse = f.run(q, n * block, None, idx, cnt)
+    check(f, q, o, lse, [n * block], d ** -0.5, kept)
+
+
+@pytest.mark.parametrize("t", [2, 3])
+def test_nan_scale_in_tiles(M, t):
+    """A NaN scale of a listed block in the kernel for many rows: NaN in the
+    rows that list it, in no others, and a NaN value scale leaves the lse."""
+    d, block, n, Lq = 128, 128, 5, 300
+    f = Filled(M, 1, 2, n * block, d, block, R.INT8, [n * block])
+    q = queries(1, 2, Lq, d, 1)
+    idx = torch.zeros((1, 2, 3, n), dtype=torch.int32)
+    idx[0, 0] = torch.arange(n)
+    idx[0, 1] = torch.tensor([0, 1, 3, 4, 2])
+    cnt = torch.tensor([5, 4], dtype=torch.int32).view(1, 2, 1).expand(1, 2, 3).contiguous()
+    o0, lse0 = f.run(q, n * block, None, idx, cnt)
+    f.dev[t][0, :, 2] = math.nan
+    o, lse = f.run(q, n * block, None, idx, cnt)
+    assert o[0, 0].isnan().all() and torch.equal(o[0, 1], o0[0, 1]) and torch.equal(lse[0, 1], lse0[0, 1])
+    assert lse[0, 0].isnan().all() if t == 2 else torch.all((lse[0, 0] - lse0[0, 0]).abs() <= 1e-5)
+    # and without lists, where every row reads it
+    o, lse = f.run(q, n * block)
+    assert o.isnan().all()
+
+
+def test_strided_views_and_shared_tensors(M):
+    """Two calls at once on two streams with a workspace each, and the same
+    call on both formats' caches, leave each other alone; q, o and lists that
+    are not contiguous are refused."""
+    f = Filled(M, 2, 2, 5000, 128, 128, R.E4M3, [5000, 4000], seed=4)
+    lens = torch.tensor([5000, 4000], dtype=torch.int32)
+    qs = [queries(2, 4, 3, 128, s) for s in (1, 2)]
+    want = [f.run(q, 5000, lens) for q in qs]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    qd, ld = [q.cuda() for q in qs], lens.cuda()
+    outs = [torch.empty_like(q) for q in qd]
+    need = M.mod_cache_attn_workspace_bytes(f.shape, 4, 3, 5000)
+    wss = [torch.full((need,), 255, dtype=torch.uint8).cuda() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, q, o, ws in zip(streams, qd, outs, wss):
+            M.mod_cache_attn_fwd(f.shape, f.ref, q, 5000, ld, None, None, 0.0, o, None, ws, need, stream=s)
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert torch.equal(o, w[0])
+    bad = torch.empty((2, 3, 4, 128), dtype=torch.bfloat16).cuda().transpose(1, 2)
+    for q, o in ((bad, outs[0]), (qd[0], bad)):
+        with pytest.raises(ValueError):
+            M.mod_cache_attn_fwd(f.shape, f.ref, q, 5000, ld, None, None, 0.0, o)
