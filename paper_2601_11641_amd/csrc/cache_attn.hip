@@ -8,10 +8,18 @@
 // running maximum and sum of the softmax (in units of log 2) and the output
 // accumulate in fp32.
 //
-// rows_kernel: a work item is (sequence, head, tile of 16 RT query rows, part
-// of the walk over the tokens); its four waves take steps of 32 tokens in turn,
-// each with a softmax state of its own, and are joined at the end.  A wave
-// keeps everything in registers:
+// A call is cut into items: (sequence, head, tile of query rows, part of the
+// walk over its tokens).  Two kernels take them by the rows of a tile, and
+// join_kernel joins the parts of a walk:
+//   rows_kernel   up to 32 rows (64 with lists): bound by reading the cache;
+//   tile_kernel   128 or 256 rows: bound by the matrix cores' power.
+// Without lists the query heads of a key/value head share a tile (their rows
+// are consecutive in memory).
+//
+// rows_kernel: the waves of a work-group take steps of 32 tokens in turn, each
+// with a softmax state of its own, and are joined at the end.  A wave keeps
+// everything in registers, without LDS or a barrier in its loop, and has the
+// codes of its next step under way while it computes one:
 //   S^T (tokens x rows) = K Q^T   v_mfma_f32_16x16x32_bf16: a lane loads 16
 //       consecutive bytes of one token's K; which channels meet in a matrix
 //       step is free as long as Q is laid out alike;
@@ -19,8 +27,9 @@
 //       belong to are those whose V it loads (D/16 consecutive channels
 //       each), so P needs no exchange between lanes and V^T is formed by
 //       byte permutes of the lane's own loads.
-// No LDS and no barrier in the loop.  Without lists the query heads of a
-// key/value head share the item (their rows are consecutive in memory).
+// One query over 24 heads of 118,800 tokens of 128 channels (730 MB) takes 132
+// us: 5.5 TB/s, where a large copy moves 4.9.  With one step's codes and no
+// more under way it took 177 us.
 #include "moddit_internal.h"
 
 #include <algorithm>
@@ -409,11 +418,21 @@ __global__ __launch_bounds__(64 * kRowWaves<RT>, 1) void rows_kernel(AttnArgs a)
 //             wants it in),
 //   product   O^T += V^T P^T of the half before that,
 // with v_mfma_f32_32x32x16_bf16; V^T comes from the row-major tile through
-// transposing LDS reads.  A wave issues an instruction every eight cycles at
-// most and a matrix instruction takes 32, so the matrix instructions of a half
+// transposing LDS reads.  A wave issues an instruction every five cycles or so
+// and a matrix instruction takes 32, so the matrix instructions of a half
 // ("slots") are spaced out by its vector instructions: the softmax, and the
 // conversion of the codes of the next unit, which were loaded one unit earlier.
 // K and V tiles are double-buffered, V one unit behind K: one barrier a unit.
+// With 256 rows one work-group fills a compute unit, with 128 two share it.
+//
+// 10,800 queries over 24 heads of 118,800 tokens (15.8 TFLOP): int8 15.3 ms,
+// 1.03 PFLOP/s (e4m3 1.09), where a bf16 matrix product of 8192 reaches 1.28.
+// The clock falls as the matrix cores are kept busier (47% of the cycles at 2.0
+// GHz), so what is left is energy, not stalls: three buffers with the barrier
+// off the critical path saved 6% of the cycles and no time, reads further
+// ahead, priorities and other orders of a half nothing.  Phases of scores and
+// softmax behind barriers took 17.1 ms, rows_kernel alone 28.6; unrolling the
+// loop by buffer spilled and took 35.
 // ---------------------------------------------------------------------------
 constexpr int kUnit = 64;
 
@@ -893,10 +912,15 @@ Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool l
     const int rows = lists ? std::min(block, Lq) : (int)std::min<long>((long)(Hq / H) * Lq, 1L << 30);
     Plan best{};
     double least = 0.0;
-    // Work-groups run in rounds: the form and the number of parts whose rounds
-    // end first.  A part costs a start, and its partial results are written and
-    // read.  The length of lists is not known here: they are taken to keep a
-    // quarter.
+    // Work-groups run in rounds; the parts of a walk are chosen, and between 128
+    // and 256 rows the form, so that the rounds end first by this estimate in
+    // microseconds.  The lengths of lists are not known here: they are taken to
+    // keep a quarter.  What the choice does: one query over 24 heads of 118,800
+    // tokens 648 us whole, 207 in 4 parts, 132 in 10 (240 work-groups, taken),
+    // 148 in 16; 8 heads of 8192 46 us whole, 9.7 in 32 parts (taken); 4 x 8
+    // heads of 32768 172 us whole, 45 in 8.  One frame of 3600 queries over 24
+    // heads' lists is 696 tiles of 128, two rounds, the second short: 1.50 ms
+    // whole, 1.42 in the two parts taken.
     auto consider = [&](int tile) {
         Plan p;
         p.rows = tile;
@@ -910,29 +934,34 @@ Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool l
         const int turn = small ? kStep * (tile == 64 ? kRowWaves<4> : kRowWaves<1>) : kUnit;
         const double walk = std::max(1.0, (lists ? 0.25 : 1.0) * max_len / turn);
         const double exist = (double)std::min(tile, rows);
-        for (int c = 1; c <= 256 && (c == 1 || walk / c >= 1.0); ++c) {
+        auto weigh = [&](int c) {
             const long items = (long)p.units * c;
-            if (c > 1 && items > (1L << 18)) break;      // (and a launch's work-groups keep to their limit)
-            p.C = c;
+            if (c > 1 && (c > walk || items > (1L << 18))) return;   // (a launch's work-groups keep to their limit)
             const double rounds = (double)((items + slots - 1) / slots);
-            // microseconds of a turn (the loads' latency, or the share of 5.5 TB/s
-            // that the resident work-groups leave to one; products and softmax), of
-            // a start, and of a join (a launch; its partial results at 4.5 TB/s)
+            // a turn (the loads' latency, and the share of the bandwidth that the
+            // resident work-groups leave to one; or products and softmax), a start,
+            // a join (its launch, and the partial results at 4.5 TB/s both ways)
             const double us = small ? 1.0 + 2.0 * turn * d * std::min<long>(items, slots) / 8.5e6
-                                    : (tile == 128 ? 2.3 : 2.1) * (items <= 256 && tile == 128 ? 0.7 : 1.0);
+                                    : tile == 128 ? (items <= 256 ? 1.6 : 2.3) : 2.1;
             const double start = small ? 3.0 : 8.0;
             const double join = c == 1 ? 0.0 : 5.0 + 0.02 * c + 8.0 * items * exist * d / 4.5e6;
             const double cost = rounds * (walk / c * us + start) + join;
             if (least == 0.0 || cost < least) {
                 least = cost;
                 best = p;
+                best.C = c;
             }
-        }
+        };
+        // whole, a few parts, and the most that one, two ... rounds hold
+        for (int c = 1; c <= 8; ++c) weigh(c);
+        for (int r = 1; r <= 8; ++r) weigh(std::max(1, std::min({(int)walk, 256, r * slots / p.units})));
     };
     if (rows <= 16) consider(16);
     else if (rows <= 32) consider(32);
     else if (rows <= 64 && lists) consider(64);
     else {
+        // 33 to 64 rows without lists: half a tile of 128 is empty, but 64 queries
+        // over 24 x 118,800 tokens take 243 us so and 323 in rows_kernel
         consider(128);
         if (!lists && rows > 128) consider(256);
     }
