@@ -409,8 +409,9 @@ size_t mod_cache_attn_workspace_bytes(const mod_cache_shape* shape, int Hq, int 
  * sequence's end are skipped, each block is listed at most once.
  * A row that keeps no token gives O = 0 and lse = -inf.  scale = 0 means
  * 1/sqrt(d).  q, k and v enter bf16 MFMA products without error (every code is
- * a bf16 number); probabilities, times the value scale, are rounded to bf16;
- * sums, softmax and accumulation are fp32.  The result does not depend on
+ * a bf16 number); probabilities, times the value scale, are rounded to bf16 (to
+ * two bf16, about 2^-17, where a head's rows are at most 16); sums, softmax and
+ * accumulation are fp32.  The result does not depend on
  * anything outside the sequence's own tokens, and is the same in every run. */
 mod_status mod_cache_attn_fwd(const mod_cache_shape* shape, const mod_cache* cache, const void* q, int Hq, int Lq,
                               int max_len, const int32_t* kv_len, const int32_t* kv_idx, const int32_t* kv_cnt,

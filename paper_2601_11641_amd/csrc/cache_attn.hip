@@ -4,7 +4,8 @@
 // with one s_k and s_v per block of tokens and head.  Every code is exactly a
 // bf16 number, so the products run on bf16 matrix instructions without any
 // rounding of K, V or Q: s_k is a factor of the scores of a block, s_v one of
-// its probabilities, which are rounded to bf16 once after it.  Scores, the
+// its probabilities, which are rounded to bf16 once after it (with up to 16
+// rows to two bf16, hardly at all).  Scores, the
 // running maximum and sum of the softmax (in units of log 2) and the output
 // accumulate in fp32.
 //
@@ -185,6 +186,11 @@ __device__ __forceinline__ bool item_of(const AttnArgs& a, int& unit, int& part)
 template <int D, int FMT, int RT, bool LISTS>
 __global__ __launch_bounds__(64 * kRowWaves<RT>, 1) void rows_kernel(AttnArgs a) {
     constexpr int ROWS = 16 * RT, WAVES = kRowWaves<RT>;
+    // With 16 rows the memory bounds the kernel: P enters as two bf16, its
+    // rounding and what that left off, so that the output's own rounding is the
+    // only one that counts (132 -> 133 us on 24 heads of 118,800 tokens; 52 -> 56
+    // us with 32 rows, four sequences of 32768, where P is one bf16).
+    constexpr bool TWICE = RT == 1;
     constexpr int KC = D / 64;          // 16-byte chunks of a token's K per lane
     constexpr int VF = D / 16;          // channels of V per lane, 16-channel tiles of O^T
     constexpr int VW = VF / 4;          // dwords of V per token and lane
@@ -301,7 +307,7 @@ __global__ __launch_bounds__(64 * kRowWaves<RT>, 1) void rows_kernel(AttnArgs a)
                     st[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                         kf, qf[rt][c], c == 0 ? f32x4{0, 0, 0, 0} : st[rt][t], 0, 0, 0);
             }
-        bf16x8 pf[RT];
+        bf16x8 pf[RT], pl[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             float x[8], mx = -INFINITY;
@@ -328,6 +334,7 @@ __global__ __launch_bounds__(64 * kRowWaves<RT>, 1) void rows_kernel(AttnArgs a)
                 const float p = __builtin_amdgcn_exp2f(x[e] - mb);
                 l[rt] += p;
                 pf[rt][e] = static_cast<__bf16>(p * y.vs);
+                if constexpr (TWICE) pl[rt][e] = static_cast<__bf16>(p * y.vs - static_cast<float>(pf[rt][e]));
             }
         }
         static_for<VF>([&](auto f_tag) __attribute__((always_inline)) {
@@ -336,8 +343,10 @@ __global__ __launch_bounds__(64 * kRowWaves<RT>, 1) void rows_kernel(AttnArgs a)
                              column_pair<FMT, BY>(y.v[4][W], y.v[5][W]), column_pair<FMT, BY>(y.v[6][W], y.v[7][W])};
             const bf16x8 vf = __builtin_bit_cast(bf16x8, x);
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
+            for (int rt = 0; rt < RT; ++rt) {
                 acc[rt][F] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rt], acc[rt][F], 0, 0, 0);
+                if constexpr (TWICE) acc[rt][F] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[rt], acc[rt][F], 0, 0, 0);
+            }
         });
     };
     while (s < s1) {
