@@ -12,8 +12,8 @@
 // A call is cut into items: (sequence, head, tile of query rows, part of the
 // walk over its tokens).  Two kernels take them by the rows of a tile, and
 // join_kernel joins the parts of a walk:
-//   rows_kernel   up to 32 rows (64 with lists): bound by reading the cache;
-//   tile_kernel   128 or 256 rows: bound by the matrix cores' power.
+//   rows_kernel   up to 32 rows: bound by reading the cache;
+//   tile_kernel   64, 128 or 256 rows: bound by the matrix cores' power.
 // Without lists the query heads of a key/value head share a tile (their rows
 // are consecutive in memory).
 //
@@ -64,9 +64,9 @@ __device__ __forceinline__ void static_for(F&& f) {
     static_for_impl(f, std::make_integer_sequence<int, N>{});
 }
 
-// Waves of a work-group of rows_kernel, by its row tiles of 16.
-template <int RT>
-constexpr int kRowWaves = RT == 4 ? 4 : 8;
+constexpr int kRowWaves = 8;       // waves of a work-group of rows_kernel
+template <int ROWS>
+constexpr int kTileWaves = ROWS == 256 ? 8 : 4;   // of tile_kernel
 
 struct AttnArgs {
     const uint16_t* q;
@@ -184,8 +184,8 @@ __device__ __forceinline__ bool item_of(const AttnArgs& a, int& unit, int& part)
 }
 
 template <int D, int FMT, int RT, bool LISTS>
-__global__ __launch_bounds__(64 * kRowWaves<RT>, 1) void rows_kernel(AttnArgs a) {
-    constexpr int ROWS = 16 * RT, WAVES = kRowWaves<RT>;
+__global__ __launch_bounds__(64 * kRowWaves, 1) void rows_kernel(AttnArgs a) {
+    constexpr int ROWS = 16 * RT, WAVES = kRowWaves;
     // With 16 rows the memory bounds the kernel: P enters as two bf16, its
     // rounding and what that left off, so that the output's own rounding is the
     // only one that counts (132 -> 133 us on 24 heads of 118,800 tokens; 52 -> 56
@@ -418,10 +418,10 @@ __global__ __launch_bounds__(64 * kRowWaves<RT>, 1) void rows_kernel(AttnArgs a)
 }
 
 // ---------------------------------------------------------------------------
-// tile_kernel: tiles of 32 WAVES query rows of a head, for calls with many rows.
+// tile_kernel: tiles of 64, 128 or 256 query rows of a head, for calls with more.
 // The work-group brings the walk's tokens into LDS as bf16, 64 at a time (a
 // "unit"), so a code is converted once for all rows of the tile; a wave owns 32
-// rows.  It works on halves of a unit (32 tokens) as a pipeline of three:
+// rows (64-row tiles: two waves do, each half of the tokens).  It works on halves of a unit (32 tokens) as a pipeline of three:
 //   scores    S^T (32 tokens x 32 rows) = K Q^T of one half,
 //   softmax   of the half before it (P stays in the lanes that the product
 //             wants it in),
@@ -457,9 +457,10 @@ struct Unit {
     int valid;      // tokens of the unit that exist
 };
 
-template <int D, int FMT, bool LISTS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
-    constexpr int ROWS = 32 * WAVES;
+template <int D, int FMT, bool LISTS, int ROWS>
+__global__ __launch_bounds__(64 * kTileWaves<ROWS>, 2) void tile_kernel(AttnArgs a) {
+    constexpr int WAVES = kTileWaves<ROWS>;
+    constexpr bool SPLIT = ROWS == 64;           // two waves to 32 rows, each its half of every unit
     constexpr int DT = D / 32, KK = D / 16;
     constexpr int SLOTS = KK + 2 * DT;           // matrix instructions of a half
     // LDS rows of K are 16 bytes longer than their 2 D bytes, so that the 16 rows
@@ -480,6 +481,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int qw = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l32 = lane & 31, h = lane >> 5;
+    const int th = SPLIT ? qw >> 1 : 0;          // the wave's half of the units
     const Rows r = rows_of<ROWS, LISTS>(a, unit);
     if (r.count <= 0) return;                    // a tile past a short query block
 
@@ -500,7 +502,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
     const int u0 = (int)((long)steps * part / a.C);
     const int T = __builtin_amdgcn_readfirstlane((int)((long)steps * (part + 1) / a.C) - u0);   // units of this item
 
-    const int row = 32 * qw + l32;               // the lane's row of the tile
+    const int row = 32 * (SPLIT ? qw & 1 : qw) + l32;   // the lane's row of the tile
     bf16x8 qreg[KK];
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
@@ -517,8 +519,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
     // LDS addresses of the operands in the first buffers
     const uint32_t lds0 = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)lds;
     const int s16 = lane & 15;
-    const uint32_t kad = lds0 + (uint32_t)(l32 * KROW + 16 * h);
-    const uint32_t vad = lds0 + (uint32_t)(2 * KTILE + (4 * h + (s16 >> 2)) * VROW + 32 * (lane >> 4 & 1) + 8 * (s16 & 3));
+    const uint32_t kad = lds0 + (uint32_t)((32 * th + l32) * KROW + 16 * h);
+    const uint32_t vad = lds0 + (uint32_t)(2 * KTILE + (32 * th + 4 * h + (s16 >> 2)) * VROW + 32 * (lane >> 4 & 1) + 8 * (s16 & 3));
 
     // staging: thread tid brings a piece of a token's codes, one or two 16-byte
     // chunks of its LDS row
@@ -639,7 +641,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
         constexpr int EPS = 16 / SLOTS;          // scores of a lane per slot
         float sc = u.sc;
         if constexpr (SM) {
-            const int lim = u.valid - 32 * PS;
+            const int lim = u.valid - 32 * (SPLIT ? th : PS);
             if (lim < 32) {
                 const int mine = lim - 4 * h;
 #pragma unroll
@@ -753,9 +755,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
         return Unit{uniform(ks * a.c2), uniform(plain ? __builtin_amdgcn_logf(vs) : 0.0f),
                     uniform(plain ? __builtin_amdgcn_rcpf(vs) : 1.0f), t0 < 0 ? 0 : len - t0};
     };
-    int tn = -1, jn = 0;                         // the next unit's first token, list entry of the one after
-
-    float ks = 1.0f, vs = 1.0f;
+    // first tokens of this unit and the next, list entry of the one after
+    int tc = -1, tn = -1, jn = 0;
+    float ks = 1.0f, vs = 1.0f, vnow = 1.0f;
     Unit before{}, now{};
     // One unit, its K at kc and the V of the unit before at vp: its scores, the
     // rest of the unit before, and half of its softmax.
@@ -787,8 +789,84 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
         kc = kn;
         vp = vc;
     };
-    if (T > 0) {
-        const int tc = token_of(0, entry_of(0));
+    if constexpr (SPLIT) {
+        // Here the pipeline runs over units: step j takes the scores of unit j, the
+        // softmax of j - 1 and the product of j - 2 (units before the first and
+        // past the last count as masked), from and into buffers j % 2, and
+        // converts K of j + 1 and V of j - 1 into the others.
+        auto step = [&](int j, auto sub_tag) __attribute__((always_inline)) {
+            constexpr int SUB = decltype(sub_tag)::value, OTHER = 1 - SUB;
+            char* const vto = vst + OTHER * VTILE;
+            float ksn, vsn;
+            fetch_scales(tn, ksn, vsn);
+            half(sub_tag, kad + SUB * KTILE, vad + SUB * VTILE, Yes{}, Yes{}, Yes{}, Yes{}, Yes{}, No{}, before,
+                 kst + OTHER * KTILE, vto, 0, 0);
+            if (!(vs >= 0x1p-64f && vs <= 0x1p64f)) stage_scaled(vto, vs);
+            load(vcodes, tc, vr);
+            int tnn = -1;
+            if (j + 2 < T) {
+                tnn = token_of(j + 2, jn);
+                load(kcodes, tnn, kr);
+                if (j + 3 < T) jn = entry_of(j + 3);
+            }
+            barrier();
+            read_ahead(kad + OTHER * KTILE, vad + OTHER * VTILE);
+            before = now;
+            vs = vnow;
+            now = unit_of(tn, ksn, vsn);
+            vnow = uniform(vsn);
+            tc = tn;
+            tn = tnn;
+        };
+        if (T > 0) {
+            for (int i = tid; i < 2 * VTILE / 16; i += 64 * WAVES)     // (P of no unit is 0, and so has V to be)
+                *reinterpret_cast<uint4*>(lds + 2 * KTILE + 16 * i) = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) pf[0][c] = pf[1][c] = u32x4{0, 0, 0, 0};
+            sacc[1] = f32x16{};
+            tc = token_of(0, entry_of(0));
+            load(kcodes, tc, kr);
+            fetch_scales(tc, ks, vnow);
+            now = unit_of(tc, ks, vnow);
+            vnow = uniform(vnow);
+            before = Unit{0.0f, 0.0f, 1.0f, 0};
+            static_for<PAIRS>([&](auto q) __attribute__((always_inline)) { convert(q, KR{}, kr, kst, kconv); });
+            if (T > 1) {
+                tn = token_of(1, entry_of(1));
+                load(kcodes, tn, kr);
+            }
+            load(vcodes, -1, vr);
+            if (T > 2) jn = entry_of(2);
+            barrier();
+            read_ahead(kad, vad);
+            for (int j = 0; j < T + 2; j += 2) {
+                step(j, I0{});
+                step(j + 1, I1{});
+            }
+        }
+        // join the two waves of a row: the second half's through LDS
+        l += __shfl_xor(l, 32);
+        float* const other = reinterpret_cast<float*>(lds) + (qw & 1) * (16 * DT + 2) * 64 + lane;
+        __syncthreads();
+        if (th == 1) {
+            other[0] = m;
+            other[64] = l;
+#pragma unroll
+            for (int i = 0; i < 16 * DT; ++i) other[(2 + i) * 64] = oacc[i / 16][i % 16];
+        }
+        __syncthreads();
+        if (th == 1) return;
+        const float m1 = other[0], l1 = other[64], top = fmaxf(m, m1);
+        const float w0 = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+        const float w1 = m1 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m1 - top);
+        // a half without a token adds nothing; NaN of either passes on
+        l = (l == 0.0f ? 0.0f : l * w0) + (l1 == 0.0f ? 0.0f : l1 * w1);
+        m = top;
+#pragma unroll
+        for (int i = 0; i < 16 * DT; ++i)
+            oacc[i / 16][i % 16] = oacc[i / 16][i % 16] * w0 + other[(2 + i) * 64] * w1;
+    } else if (T > 0) {
+        tc = token_of(0, entry_of(0));
         load(kcodes, tc, kr);
         fetch_scales(tc, ks, vs);
         now = unit_of(tc, ks, vs);
@@ -810,7 +888,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tile_kernel(AttnArgs a) {
     }
 
     // the lane's channels: 32 dt + 8 gq + 4 h + 0..3 of its row
-    l += __shfl_xor(l, 32);
+    if constexpr (!SPLIT) l += __shfl_xor(l, 32);
     if (row >= r.count) return;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const float lse2 = l == 0.0f ? -INFINITY : m + __builtin_amdgcn_logf(l);
@@ -913,7 +991,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
 
 // How a call is cut up, from its host sizes alone.
 struct Plan {
-    int rows;                  // rows of a tile: 16, 32, 64 (rows_kernel), 128, 256 (tile_kernel)
+    int rows;                  // rows of a tile: 16, 32 (rows_kernel), 64, 128, 256 (tile_kernel)
     int C;                     // parts of a walk
     int tiles, heads, units;
 };
@@ -936,11 +1014,11 @@ Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool l
         p.tiles = (rows + tile - 1) / tile;
         p.heads = lists ? Hq : H;
         p.units = B * p.heads * (lists ? (Lq + block - 1) / block : 1) * p.tiles;
-        const bool small = tile <= 64;
+        const bool small = tile <= 32;
         // resident work-groups; tokens of one turn of a work-group (a step of all
         // its waves, a unit)
-        const int slots = tile == 128 ? 512 : 256;
-        const int turn = small ? kStep * (tile == 64 ? kRowWaves<4> : kRowWaves<1>) : kUnit;
+        const int slots = small || tile == 256 ? 256 : 512;
+        const int turn = small ? kStep * kRowWaves : kUnit;
         const double walk = std::max(1.0, (lists ? 0.25 : 1.0) * max_len / turn);
         const double exist = (double)std::min(tile, rows);
         auto weigh = [&](int c) {
@@ -951,7 +1029,7 @@ Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool l
             // resident work-groups leave to one; or products and softmax), a start,
             // a join (its launch, and the partial results at 4.5 TB/s both ways)
             const double us = small ? 1.0 + 2.0 * turn * d * std::min<long>(items, slots) / 8.5e6
-                                    : tile == 128 ? (items <= 256 ? 1.6 : 2.3) : 2.1;
+                                    : tile == 256 ? 2.1 : (tile == 64 ? 0.6 : 1.0) * (items <= 256 ? 1.6 : 2.3);
             const double start = small ? 3.0 : 8.0;
             const double join = c == 1 ? 0.0 : 5.0 + 0.02 * c + 8.0 * items * exist * d / 4.5e6;
             const double cost = rounds * (walk / c * us + start) + join;
@@ -967,10 +1045,8 @@ Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool l
     };
     if (rows <= 16) consider(16);
     else if (rows <= 32) consider(32);
-    else if (rows <= 64 && lists) consider(64);
+    else if (rows <= 64) consider(64);
     else {
-        // 33 to 64 rows without lists: half a tile of 128 is empty, but 64 queries
-        // over 24 x 118,800 tokens take 243 us so and 323 in rows_kernel
         consider(128);
         if (!lists && rows > 128) consider(256);
     }
@@ -984,10 +1060,10 @@ template <int D, int FMT, int ROWS, bool LISTS>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
     const int round = kXcds * a.stretch;
     const dim3 grid((unsigned)((a.units * a.C + round - 1) / round * round));
-    if constexpr (ROWS >= 128)
-        hipLaunchKernelGGL((tile_kernel<D, FMT, LISTS, ROWS / 32>), grid, dim3(2 * ROWS), 0, s, a);
+    if constexpr (ROWS >= 64)
+        hipLaunchKernelGGL((tile_kernel<D, FMT, LISTS, ROWS>), grid, dim3(64 * kTileWaves<ROWS>), 0, s, a);
     else
-        hipLaunchKernelGGL((rows_kernel<D, FMT, ROWS / 16, LISTS>), grid, dim3(64 * kRowWaves<ROWS / 16>), 0, s, a);
+        hipLaunchKernelGGL((rows_kernel<D, FMT, ROWS / 16, LISTS>), grid, dim3(64 * kRowWaves), 0, s, a);
     if (a.C > 1) {
         auto join = [&](auto slices) {
             constexpr int SL = decltype(slices)::value, RPG = 256 / (D / 4 * SL);
@@ -1022,9 +1098,7 @@ hipError_t launch_cache_attn(const CacheView& c, const uint16_t* q, int Hq, int 
         constexpr bool LISTS = decltype(ls)::value;
         if (p.rows == 16) e = launch<D, FMT, 16, LISTS>(a, s);
         else if (p.rows == 32) e = launch<D, FMT, 32, LISTS>(a, s);
-        else if (p.rows == 64) {
-            if constexpr (LISTS) e = launch<D, FMT, 64, LISTS>(a, s);
-        }
+        else if (p.rows == 64) e = launch<D, FMT, 64, LISTS>(a, s);
         else if (p.rows == 128) e = launch<D, FMT, 128, LISTS>(a, s);
         else if constexpr (!LISTS) e = launch<D, FMT, 256, LISTS>(a, s);
     };
