@@ -432,7 +432,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void rows_kernel(AttnArgs a) {
 // ("slots") are spaced out by its vector instructions: the softmax, and the
 // conversion of the codes of the next unit, which were loaded one unit earlier.
 // K and V tiles are double-buffered, V one unit behind K: one barrier a unit.
-// With 256 rows one work-group fills a compute unit, with 128 two share it.
+// With 256 rows one work-group fills a compute unit, with fewer two share it
+// (three at d = 64).
 //
 // 10,800 queries over 24 heads of 118,800 tokens (15.8 TFLOP): int8 15.3 ms,
 // 1.03 PFLOP/s (e4m3 1.09), where a bf16 matrix product of 8192 reaches 1.28.
@@ -469,11 +470,10 @@ __global__ __launch_bounds__(64 * kTileWaves<ROWS>, 2) void tile_kernel(AttnArgs
     // instead would need an address register per operand of a half.)
     constexpr int KROW = 2 * D + 16, VROW = 2 * D + 64;
     constexpr int KTILE = kUnit * KROW, VTILE = kUnit * VROW;
-    constexpr int CPT = D / WAVES;               // codes of a tile that a thread brings: in pieces of
-    constexpr int PIECE = CPT < 16 ? CPT : 16;   // one load,
+    constexpr int CPT = D / WAVES;               // codes of a tile that a thread brings:
+    constexpr int PIECE = 16, PW = PIECE / 4;    // in pieces of one load,
     constexpr int NP = CPT / PIECE;              // each of a token TPP after the other's
     constexpr int TPR = D / PIECE, TPP = 64 * WAVES / TPR;
-    constexpr int PW = PIECE / 4;                // dwords of a piece
     __shared__ __align__(1024) char lds[2 * KTILE + 2 * VTILE];   // K, K, V, V
 
     int unit, part;
@@ -522,8 +522,8 @@ __global__ __launch_bounds__(64 * kTileWaves<ROWS>, 2) void tile_kernel(AttnArgs
     const uint32_t kad = lds0 + (uint32_t)((32 * th + l32) * KROW + 16 * h);
     const uint32_t vad = lds0 + (uint32_t)(2 * KTILE + (32 * th + 4 * h + (s16 >> 2)) * VROW + 32 * (lane >> 4 & 1) + 8 * (s16 & 3));
 
-    // staging: thread tid brings a piece of a token's codes, one or two 16-byte
-    // chunks of its LDS row
+    // staging: thread tid brings 16 codes of a token, two 16-byte chunks of its
+    // LDS row
     const int scol = tid % TPR, srow = tid / TPR;
     char* const kst = lds + srow * KROW + 2 * PIECE * scol;
     char* const vst = lds + 2 * KTILE + srow * VROW + 2 * PIECE * scol;
@@ -550,13 +550,8 @@ __global__ __launch_bounds__(64 * kTileWaves<ROWS>, 2) void tile_kernel(AttnArgs
         for (int i = 0; i < NP; ++i) {
             const int t = min(srow + TPP * i, len - 1 - t0);       // rows past the end: masked
             const uint32_t off = (uint32_t)(t * D + PIECE * scol);
-            if constexpr (PW == 4) {
-                const uint4 v = *reinterpret_cast<const uint4*>(base + off);
-                x[i][0] = v.x, x[i][1] = v.y, x[i][2] = v.z, x[i][3] = v.w;
-            } else {
-                const uint2 v = *reinterpret_cast<const uint2*>(base + off);
-                x[i][0] = v.x, x[i][1] = v.y;
-            }
+            const uint4 v = *reinterpret_cast<const uint4*>(base + off);
+            x[i][0] = v.x, x[i][1] = v.y, x[i][2] = v.z, x[i][3] = v.w;
         }
     };
     auto fetch_scales = [&](int t0, float& ks, float& vs) __attribute__((always_inline)) {
@@ -1017,7 +1012,7 @@ Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool l
         const bool small = tile <= 32;
         // resident work-groups; tokens of one turn of a work-group (a step of all
         // its waves, a unit)
-        const int slots = small || tile == 256 ? 256 : 512;
+        const int slots = small || tile == 256 ? 256 : d == 64 ? 768 : 512;
         const int turn = small ? kStep * kRowWaves : kUnit;
         const double walk = std::max(1.0, (lists ? 0.25 : 1.0) * max_len / turn);
         const double exist = (double)std::min(tile, rows);
@@ -1047,8 +1042,11 @@ Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool l
     else if (rows <= 32) consider(32);
     else if (rows <= 64) consider(64);
     else {
+        // d = 64: three work-groups of 128 rows share a compute unit and one of 256
+        // leaves a third of it empty (10,800 queries, 24 x 118,800 tokens 9.2 ms,
+        // 10.0 with 256 rows; d = 128, int8 16.2 with 256, 17.6 with 128)
         consider(128);
-        if (!lists && rows > 128) consider(256);
+        if (!lists && rows > 128 && d == 128) consider(256);
     }
     return best;
 }
@@ -1100,7 +1098,7 @@ hipError_t launch_cache_attn(const CacheView& c, const uint16_t* q, int Hq, int 
         else if (p.rows == 32) e = launch<D, FMT, 32, LISTS>(a, s);
         else if (p.rows == 64) e = launch<D, FMT, 64, LISTS>(a, s);
         else if (p.rows == 128) e = launch<D, FMT, 128, LISTS>(a, s);
-        else if constexpr (!LISTS) e = launch<D, FMT, 256, LISTS>(a, s);
+        else if constexpr (!LISTS && D == 128) e = launch<D, FMT, 256, LISTS>(a, s);
     };
     auto with_fmt = [&](auto d, auto fmt) {
         if (lists) with_rt(d, fmt, std::true_type{});
