@@ -323,7 +323,7 @@ mod_status mod_rope_destroy(mod_rope* rope);
  * text_tokens tokens have no position and are copied.  The rotated channels of
  * a token whose position is outside [0, frames*height*width) become NaN (with
  * starts NULL: MOD_ERR_INVALID_ARG).  y may be x where the strides are equal; they must not
- * overlap otherwise. */
+ * overlap otherwise (nor y's own rows). */
 mod_status mod_rope_fwd(const mod_rope* rope, const mod_shape* shape, const void* x, const mod_strides* x_strides,
                         void* y, const mod_strides* y_strides, int first, const int32_t* starts, void* stream);
 
@@ -349,7 +349,8 @@ typedef struct {
 
 /* Device memory of the caller: codes [B, H, capacity, d], one byte each,
  * 16-byte aligned, and scales [B, H, mod_cache_blocks(shape)].  Needs no
- * initial values. */
+ * initial values where every sequence's tokens are written in order from its
+ * position 0 on. */
 typedef struct {
     void* k;
     void* v;
@@ -383,15 +384,17 @@ mod_status mod_cache_write(const mod_cache_shape* shape, const mod_cache* cache,
                            const mod_strides* k_strides, const void* v, const mod_strides* v_strides, int L,
                            int first, const int32_t* starts, const int32_t* counts, void* stream);
 
-/* What the tokens at those positions stand for, code * scale rounded to bf16
- * once.  Rows of tokens that mod_cache_write would not write are left as they
+/* What the tokens at those positions stand for: code * scale in fp32 (exact for
+ * E4M3), rounded to bf16.  Rows of tokens that mod_cache_write would not write are left as they
  * were.  k or v may be NULL (not read). */
 mod_status mod_cache_read(const mod_cache_shape* shape, const mod_cache* cache, void* k, const mod_strides* k_strides,
                           void* v, const mod_strides* v_strides, int L, int first, const int32_t* starts,
                           const int32_t* counts, void* stream);
 
-/* Workspace of mod_cache_attn_fwd in bytes, for at most max_len cached tokens
- * (0: none needed, or an invalid argument).  Owned by the caller; two calls in
+/* Workspace in bytes of a mod_cache_attn_fwd with these sizes (0: none needed,
+ * or an invalid argument).  A smaller max_len can need more: a loop over a
+ * growing sequence with one workspace passes its largest max_len every time
+ * and the lengths as kv_len.  Owned by the caller; two calls in
  * flight at once (two streams, or two captured graphs) need two. */
 size_t mod_cache_attn_workspace_bytes(const mod_cache_shape* shape, int Hq, int Lq, int max_len);
 

@@ -381,7 +381,10 @@ def mod_cache_blocks(shape: mod_cache_shape) -> int:
 
 def _store_call(name, shape, cache, k, v, first, starts, counts, L, stream):
     if L is None:
-        L = (k if k is not None else v).shape[2]
+        x = k if k is not None else v
+        if x is not None and not hasattr(x, "shape"):
+            raise TypeError("L is needed where k and v are addresses")
+        L = x.shape[2] if x is not None and x.dim() == 4 else 1
     dims = (shape.B, shape.H, L, shape.d)
     kp, ks = _strided(k, dims, "k")
     vp, vs = _strided(v, dims, "v")
@@ -417,6 +420,8 @@ def mod_cache_attn_fwd(shape: mod_cache_shape, cache: mod_cache, q, max_len: int
         if q.dim() != 4 or q.shape[0] != shape.B or q.shape[3] != shape.d:
             raise ValueError(f"q must have shape ({shape.B}, Hq, Lq, {shape.d}), got {tuple(q.shape)}")
         Hq, Lq = q.shape[1], q.shape[2]
+    elif Hq is None or Lq is None:
+        raise TypeError("Hq and Lq are needed where q is an address")
     n, nq = -(-max_len // shape.block), -(-Lq // shape.block)
     B, bf16, i32 = shape.B, torch.bfloat16, torch.int32
     args = (_array(q, None, bf16, "q"), Hq, Lq, max_len, _array(kv_len, (B,), i32, "kv_len"),
@@ -426,9 +431,13 @@ def mod_cache_attn_fwd(shape: mod_cache_shape, cache: mod_cache, q, max_len: int
     if workspace is None and hasattr(q, "device"):
         ws_bytes = mod_cache_attn_workspace_bytes(shape, Hq, Lq, max_len)
         if ws_bytes > 0:
-            workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
-            if st != torch.cuda.current_stream().cuda_stream:   # its memory waits for that stream's use of it
-                workspace.record_stream(torch.cuda.ExternalStream(st))
+            if st == _stream(None):
+                workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+            else:   # of the stream that uses it: nothing else does before or after in another order
+                with torch.cuda.stream(torch.cuda.ExternalStream(st)):
+                    workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
+    elif hasattr(workspace, "nbytes") and workspace.nbytes < ws_bytes:
+        raise ValueError(f"workspace has {workspace.nbytes} bytes, ws_bytes says {ws_bytes}")
     _check(_lib.mod_cache_attn_fwd(ctypes.byref(shape), ctypes.byref(cache), *args,
                                    _array(workspace, None, None, "workspace"), ws_bytes, st), "mod_cache_attn_fwd")
 

@@ -10,6 +10,8 @@
 //          x - r s is exact in fp32 (both are multiples of the last place of
 //          s, and it is at most about s), so comparing its double with s
 //          decides the border as the real quotient does.
+// Reading multiplies in fp32 and rounds to bf16: for E4M3 the product is exact, for
+// INT8 (31 bits) its own rounding comes on top, 2^-16 of the second one.
 // Bound by memory: per channel two bytes read and one written (write), or one
 // read and two written (read).  One work-group per (sequence, head, block,
 // K or V) keeps the block's new rows in registers between the maximum and the

@@ -29,15 +29,20 @@ mod_status check_aligned(const void* p, const char* what) {
     return MOD_OK;
 }
 
-// The [B, H, L, d] tensor at p with the caller's strides.
-mod_status make_strided(const void* p, const mod_strides* st, int H, int L, int d, const char* what,
-                        moddit::Strided* out) {
+// The [B, H, L, d] tensor at p with the caller's strides; `written`: of a tensor
+// that a call writes, whose rows must not lie on each other.
+mod_status make_strided(const void* p, const mod_strides* st, int B, int H, int L, int d, bool written,
+                        const char* what, moddit::Strided* out) {
     const mod_status e = check_aligned(p, what);
     if (e != MOD_OK) return e;
     out->p = static_cast<uint16_t*>(const_cast<void*>(p));
     if (st) {
         if (st->b % 8 != 0 || st->h % 8 != 0 || st->l % 8 != 0)
             return fail(MOD_ERR_INVALID_ARG, "%s: strides must be multiples of 8 elements (b=%ld h=%ld l=%ld)", what,
+                        (long)st->b, (long)st->h, (long)st->l);
+        auto on_itself = [&](int n, int64_t stride) { return n > 1 && stride > -d && stride < d; };
+        if (written && (on_itself(B, st->b) || on_itself(H, st->h) || on_itself(L, st->l)))
+            return fail(MOD_ERR_INVALID_ARG, "%s is written: its rows must not overlap (b=%ld h=%ld l=%ld)", what,
                         (long)st->b, (long)st->h, (long)st->l);
         out->b = st->b;
         out->h = st->h;
@@ -128,11 +133,15 @@ mod_status rope_call(const mod_rope* rope, const mod_shape* shape, const void* x
                     shape->L - shape->text_tokens, first, total);
     if ((long)shape->B * ((shape->L + 15L) / 16) > kMaxGroups)
         return fail(MOD_ERR_UNSUPPORTED, "B*L too large for one call");
+    if ((long)shape->B * shape->H > kMaxHeads) return fail(MOD_ERR_UNSUPPORTED, "B*H too large");
     moddit::Strided in{}, out{};
-    mod_status st = make_strided(x, xs, shape->H, shape->L, p.d, backward ? "dy" : "x", &in);
+    mod_status st = make_strided(x, xs, shape->B, shape->H, shape->L, p.d, false, backward ? "dy" : "x", &in);
     if (st != MOD_OK) return st;
-    st = make_strided(y, ys, shape->H, shape->L, p.d, backward ? "dx" : "y", &out);
+    st = make_strided(y, ys, shape->B, shape->H, shape->L, p.d, true, backward ? "dx" : "y", &out);
     if (st != MOD_OK) return st;
+    if (in.p == out.p && ((shape->B > 1 && in.b != out.b) || (shape->H > 1 && in.h != out.h) ||
+                          (shape->L > 1 && in.l != out.l)))
+        return fail(MOD_ERR_INVALID_ARG, "a rotation in place needs the same strides on both sides");
     const hipError_t e = moddit::launch_rope(rope->view, in, out, shape->B, shape->H, shape->L, p.d,
                                              shape->text_tokens, first, starts, backward,
                                              static_cast<hipStream_t>(stream));
@@ -245,9 +254,9 @@ mod_status mod_cache_write(const mod_cache_shape* shape, const mod_cache* cache,
     st = check_range(shape, L, first, starts);
     if (st != MOD_OK) return st;
     moddit::Strided ks{}, vs{};
-    st = make_strided(k, k_strides, shape->H, L, shape->d, "k", &ks);
+    st = make_strided(k, k_strides, shape->B, shape->H, L, shape->d, false, "k", &ks);
     if (st != MOD_OK) return st;
-    st = make_strided(v, v_strides, shape->H, L, shape->d, "v", &vs);
+    st = make_strided(v, v_strides, shape->B, shape->H, L, shape->d, false, "v", &vs);
     if (st != MOD_OK) return st;
     const hipError_t e = moddit::launch_cache_write(view, ks, vs, L, first, starts, counts,
                                                     static_cast<hipStream_t>(stream));
@@ -265,9 +274,9 @@ mod_status mod_cache_read(const mod_cache_shape* shape, const mod_cache* cache, 
     st = check_range(shape, L, first, starts);
     if (st != MOD_OK) return st;
     moddit::Strided ks{}, vs{};
-    st = make_strided(k, k_strides, shape->H, L, shape->d, "k", &ks);
+    st = make_strided(k, k_strides, shape->B, shape->H, L, shape->d, true, "k", &ks);
     if (st != MOD_OK) return st;
-    st = make_strided(v, v_strides, shape->H, L, shape->d, "v", &vs);
+    st = make_strided(v, v_strides, shape->B, shape->H, L, shape->d, true, "v", &vs);
     if (st != MOD_OK) return st;
     const hipError_t e = moddit::launch_cache_read(view, ks, vs, L, first, starts, counts,
                                                    static_cast<hipStream_t>(stream));

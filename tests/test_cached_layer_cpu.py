@@ -113,6 +113,15 @@ def test_attention_refused(M, change, status):
     assert refused(M, lambda: M.mod_cache_attn_fwd(s, c, **p)) == status
 
 
+@pytest.mark.parametrize("strides", [(0, 1024, 64), (1024, 0, 64), (2048, 1024, 0), (2048, 1024, 32),
+                                     (2048, -56, 64), (-8, 1024, 64)])
+def test_read_into_overlapping_rows_refused(M, strides):
+    lib, s = M.raw_lib(), M.make_cache_shape(2, 2, 100, 64, 64)
+    c, st = M.mod_cache(A, A, A, A), ctypes.byref(M.mod_strides(*strides))
+    for ks, vs in ((st, None), (None, st)):
+        assert lib.mod_cache_read(ctypes.byref(s), ctypes.byref(c), A, ks, A, vs, 16, 0, None, None, None) == 1
+
+
 def test_attention_workspace(M):
     s, c = M.make_cache_shape(1, 2, 100000, 128, 128), M.mod_cache(A, A, A, A)
     need = M.mod_cache_attn_workspace_bytes(s, 2, 1, 100000)
@@ -121,7 +130,7 @@ def test_attention_workspace(M):
     assert refused(M, lambda: M.mod_cache_attn_fwd(s, c, workspace=A, ws_bytes=need - 1, **args)) == 1
     assert refused(M, lambda: M.mod_cache_attn_fwd(s, c, workspace=None, ws_bytes=need, **args)) == 1
     assert refused(M, lambda: M.mod_cache_attn_fwd(s, c, workspace=A + 4, ws_bytes=need, **args)) == 1
-    # a short cache needs none, and its size never shrinks what a longer one needs
+    # a short cache needs none
     assert M.mod_cache_attn_workspace_bytes(s, 2, 1, 10) == 0
     assert M.mod_cache_attn_workspace_bytes(s, 3, 1, 100) == 0 and M.mod_last_error()
 
@@ -138,6 +147,14 @@ def test_binding_checks_tensors(M):
         M.make_cache(x, x, x, x)
     with pytest.raises(ValueError):
         M.mod_cache_attn_fwd(s, c, x, 100, None, None, None, 0.0, x[:, :1], stream=0)
+    with pytest.raises(ValueError):   # a workspace smaller than its stated size
+        M.mod_cache_attn_fwd(s, c, A, 100, None, None, None, 0.0, A, None, x, x.nbytes + 1, stream=0, Hq=2, Lq=1)
+    # addresses need their sizes
+    with pytest.raises(TypeError):
+        M.mod_cache_attn_fwd(s, c, A, 100, None, None, None, 0.0, A, stream=0)
+    with pytest.raises(TypeError):
+        M.mod_cache_write(s, c, A, A, stream=0)
+    assert refused(M, lambda: M.mod_cache_read(s, c, None, None, stream=0)) == 1
 
 
 def test_struct_layouts_match_the_header(M, tmp_path):

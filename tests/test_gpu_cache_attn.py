@@ -239,6 +239,20 @@ def test_other_stream_and_no_lse(M):
     trash = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")   # would take the workspace's place
     side.synchronize()
     assert torch.equal(o, o0) and trash[0] == 255
+    # nor does it take memory that work of the current stream still writes
+    need = M.mod_cache_attn_workspace_bytes(f.shape, 2, 1, 5000)
+    assert need > 0
+    for _ in range(3):
+        big = torch.ones(4096, 4096, dtype=torch.bfloat16, device="cuda")
+        held = torch.empty(need, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        for _ in range(8):
+            big = big @ big
+        held.fill_(255)
+        del held
+        M.mod_cache_attn_fwd(f.shape, f.ref, qd, 5000, None, None, None, 0.0, o, None, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(o, o0)
 
 
 def test_captured_and_replayed(M):

@@ -5,6 +5,7 @@ import torch
 import cached_ref as R
 
 pytestmark = pytest.mark.gpu
+A = 1 << 20   # an aligned address that is never used
 
 
 @pytest.fixture(scope="module")
@@ -132,3 +133,21 @@ def test_rope_refusals_on_the_device(M):
     with pytest.raises(ValueError):
         M.mod_rope_fwd(rope.handle, M.make_shape(1, 2, 25, 64, 64, 12, 1), x, x, 0,
                        torch.zeros(2, dtype=torch.int32).cuda())
+    # a result whose rows lie on each other; in place under other strides
+    s = M.make_shape(1, 2, 24, 64, 64, 12)
+    a = torch.zeros(1, 2, 24, 64, dtype=torch.bfloat16).cuda()
+    assert status(s, a, a[:, :1].expand(1, 2, 24, 64)) == 1
+    assert status(s, a, a.view(-1).as_strided((1, 2, 24, 64), (0, 24 * 64, 32, 1))) == 1
+    assert status(s, a, a.view(1, 24, 2, 64).transpose(1, 2)) == 1
+    assert status(M.make_shape(1 << 12, 1 << 12, 1, 64, 64), A, A) == 2      # B*H
+
+
+def test_rope_of_a_broadcast_input(M):
+    d, grid = 128, (3, 4, 5)
+    rope = M.Rope(M.make_rope_params(d, (44, 42, 42), grid, pairing="halves"))
+    x = torch.randn(2, 1, 60, d).bfloat16().cuda().expand(2, 6, 60, d)
+    y, want = (torch.empty(2, 6, 60, d, dtype=torch.bfloat16).cuda() for _ in range(2))
+    shape = M.make_shape(2, 6, 60, d, 64)
+    M.mod_rope_fwd(rope.handle, shape, x, y)
+    M.mod_rope_fwd(rope.handle, shape, x.contiguous(), want)
+    assert torch.equal(y, want)
