@@ -134,6 +134,8 @@ EXPORTED = tuple(_SIGS)
 
 # the current stream's address without a stream object (0.1 us instead of 2.7)
 _current_raw_stream = getattr(getattr(torch, "_C", None), "_cuda_getCurrentRawStream", None)
+# the current device once a device tensor exists (0.07 us instead of 0.23)
+_current_device = getattr(getattr(torch, "_C", None), "_cuda_getDevice", None) or (lambda: torch.cuda.current_device())
 
 
 def _status_name(st: int) -> str:
@@ -282,8 +284,8 @@ def _device(x, what: str):
     d = x.get_device()
     if d < 0:
         raise ValueError(f"{what} must be a device tensor")
-    if d != torch.cuda.current_device():
-        raise ValueError(f"{what} is on {x.device}, but the current device is cuda:{torch.cuda.current_device()}")
+    if d != _current_device():
+        raise ValueError(f"{what} is on {x.device}, but the current device is cuda:{_current_device()}")
 
 
 def _array(x, dims, dtype, what: str):

@@ -1018,7 +1018,7 @@ Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool l
         const double exist = (double)std::min(tile, rows);
         auto weigh = [&](int c) {
             const long items = (long)p.units * c;
-            if (c > 1 && (c > walk || items > (1L << 18))) return;   // (a launch's work-groups keep to their limit)
+            if (c > 1 && items > (1L << 18)) return;   // (a launch's work-groups keep to their limit)
             const double rounds = (double)((items + slots - 1) / slots);
             // a turn (the loads' latency, and the share of the bandwidth that the
             // resident work-groups leave to one; or products and softmax), a start,
@@ -1035,8 +1035,10 @@ Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool l
             }
         };
         // whole, a few parts, and the most that one, two ... rounds hold
-        for (int c = 1; c <= 8; ++c) weigh(c);
-        for (int r = 1; r <= 8; ++r) weigh(std::max(1, std::min({(int)walk, 256, r * slots / p.units})));
+        const int most = std::min((int)walk, 256);
+        for (int c = 1; c <= std::min(most, 8); ++c) weigh(c);
+        for (int r = 1, c = 8; r <= 8 && c < most; ++r)
+            if (r * slots / p.units > 8) weigh(c = std::min(most, r * slots / p.units));
     };
     if (rows <= 16) consider(16);
     else if (rows <= 32) consider(32);
