@@ -421,7 +421,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void rows_kernel(AttnArgs a) {
 // tile_kernel: tiles of 64, 128 or 256 query rows of a head, for calls with more.
 // The work-group brings the walk's tokens into LDS as bf16, 64 at a time (a
 // "unit"), so a code is converted once for all rows of the tile; a wave owns 32
-// rows (64-row tiles: two waves do, each half of the tokens).  It works on halves of a unit (32 tokens) as a pipeline of three:
+// rows (64-row tiles: two waves do, each half of the tokens).  It works on
+// halves of a unit (32 tokens) as a pipeline of three:
 //   scores    S^T (32 tokens x 32 rows) = K Q^T of one half,
 //   softmax   of the half before it (P stays in the lanes that the product
 //             wants it in),
@@ -435,14 +436,20 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void rows_kernel(AttnArgs a) {
 // With 256 rows one work-group fills a compute unit, with fewer two share it
 // (three at d = 64).
 //
-// 10,800 queries over 24 heads of 118,800 tokens (15.8 TFLOP): int8 15.3 ms,
-// 1.03 PFLOP/s (e4m3 1.09), where a bf16 matrix product of 8192 reaches 1.28.
-// The clock falls as the matrix cores are kept busier (47% of the cycles at 2.0
+// 10,800 queries over 24 heads of 118,800 tokens (15.8 TFLOP): int8 15.0 ms,
+// 1.05 PFLOP/s (e4m3 1.09), where a bf16 matrix product of 8192 reaches 1.28.
+// The clock falls as the matrix cores are kept busier (half of the cycles at 2.0
 // GHz), so what is left is energy, not stalls: three buffers with the barrier
 // off the critical path saved 6% of the cycles and no time, reads further
-// ahead, priorities and other orders of a half nothing.  Phases of scores and
-// softmax behind barriers took 17.1 ms, rows_kernel alone 28.6; unrolling the
-// loop by buffer spilled and took 35.
+// ahead, priorities, other orders of a half and a layout without the staging
+// writes' bank conflicts (a sixth of the LDS cycles) nothing.  Phases of scores
+// and softmax behind barriers took 17.1 ms, rows_kernel alone 28.6; unrolling
+// the loop by buffer spilled and took 35.
+// 8-bit products of the codes of K with q as two E4M3 parts (exact down to 2^-21
+// of a row's largest) would save K's conversions: 5 to 9% of E4M3 calls over
+// lists.  But v_mfma_*_f8f6f4 sums 64 products with errors up to 2^-15 of their
+// magnitudes (measured; the bf16 instruction's 2^-24), and scores are sums that
+// are to hold 32 bits.
 // ---------------------------------------------------------------------------
 constexpr int kUnit = 64;
 
