@@ -316,10 +316,12 @@ def _strided(x, dims, what: str):
         raise ValueError(f"{what} must have shape {tuple(dims)}, got {tuple(x.shape)}")
     if x.dtype is not torch.bfloat16:
         raise ValueError(f"{what} must be torch.bfloat16, got {x.dtype}")
+    _device(x, what)
+    if x.is_contiguous():
+        return x.data_ptr(), None
     b, h, t, c = x.stride()
     if c != 1:
         raise ValueError(f"{what} must have contiguous channels")
-    _device(x, what)
     # the stride of an axis of one entry is of no account
     return x.data_ptr(), ctypes.byref(mod_strides(b if dims[0] > 1 else 0, h if dims[1] > 1 else 0,
                                                   t if dims[2] > 1 else 0))
