@@ -4,15 +4,15 @@
 // with one s_k and s_v per block of tokens and head.  Every code is exactly a
 // bf16 number, so the products run on bf16 matrix instructions without any
 // rounding of K, V or Q: s_k is a factor of the scores of a block, s_v one of
-// its probabilities, which are rounded to bf16 once after it (with up to 16
-// rows to two bf16, hardly at all).  Scores, the
-// running maximum and sum of the softmax (in units of log 2) and the output
-// accumulate in fp32.
+// its probabilities, which are rounded to bf16 once after it (in tiles of 16
+// rows to two bf16, hardly at all).  Scores, the running maximum and sum of the
+// softmax (in units of log 2) and the output accumulate in fp32.
 //
 // A call is cut into items: (sequence, head, tile of query rows, part of the
 // walk over its tokens).  Two kernels take them by the rows of a tile, and
 // join_kernel joins the parts of a walk:
-//   rows_kernel   up to 32 rows: bound by reading the cache;
+//   rows_kernel   16 or 32 rows: few rows, bound by reading the cache, or calls
+//                 too small to fill the chip, bound by the turns of a walk;
 //   tile_kernel   64, 128 or 256 rows: bound by the matrix cores' power.
 // Without lists the query heads of a key/value head share a tile (their rows
 // are consecutive in memory).
@@ -991,53 +991,64 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
         a.lse[r.row0 + tr] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// How a call is cut up, from its host sizes alone.
-struct Plan {
-    int rows;                  // rows of a tile: 16, 32 (rows_kernel), 64, 128, 256 (tile_kernel)
-    int C;                     // parts of a walk
-    int tiles, heads, units;
+// What an estimate of a call's time needs to know of a tile's kernel, in
+// microseconds: a turn of a work-group (a step of all its waves, a unit), what
+// each work-group per compute unit adds to it, its start and end, and how much of
+// a turn d = 64 takes.  A fit to 11,000 calls with 1 to 16,384 queries, 64 to
+// 185,000 tokens, with and without lists, each with up to 60 ways to cut it up:
+// the way chosen by it is 2 to 3% slower than the best one measured, on average.
+struct TileCost {
+    int rows;
+    double turn, more, start, half;
 };
-Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool lists) {
+constexpr TileCost kTileCosts[] = {{256, 1.4, 0.2, 7.0, 1.0},
+                                   {128, 1.4, 0.3, 6.0, 0.77},
+                                   {64, 1.2, 0.15, 9.0, 0.66},
+                                   {32, 2.5, 0.0, 6.0, 0.4},
+                                   {16, 2.2, 0.6, 5.0, 0.54}};
+
+}  // namespace
+
+CacheAttnPlan plan_cache_attn(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool lists) {
     const int rows = lists ? std::min(block, Lq) : (int)std::min<long>((long)(Hq / H) * Lq, 1L << 30);
-    Plan best{};
+    CacheAttnPlan best{};
     double least = 0.0;
-    // Work-groups run in rounds; the parts of a walk are chosen, and between 128
-    // and 256 rows the form, so that the rounds end first by this estimate in
-    // microseconds.  The lengths of lists are not known here: they are taken to
-    // keep a quarter.  What the choice does: one query over 24 heads of 118,800
-    // tokens 648 us whole, 207 in 4 parts, 132 in 10 (240 work-groups, taken),
-    // 148 in 16; 8 heads of 8192 46 us whole, 9.7 in 32 parts (taken); 4 x 8
-    // heads of 32768 172 us whole, 45 in 8.  One frame of 3600 queries over 24
-    // heads' lists is 696 tiles of 128, two rounds, the second short: 1.50 ms
+    // Work-groups run in rounds; the rows of a tile and the parts of a walk are
+    // chosen so that the rounds end first by this estimate.  The lengths of lists
+    // are not known here: they are taken to keep a quarter.  What the choice does:
+    // one query over 24 heads of 118,800 tokens 648 us whole, 207 in 4 parts, 132
+    // in 10 (240 work-groups, taken), 148 in 16; 8 heads of 8192 46 us whole, 9.7 in
+    // 32 parts (taken).  1024 queries over 8 heads of 1024: 18 us in tiles of 32
+    // (taken), 23 in tiles of 128 and three parts.  One frame of 3600 queries over
+    // 24 heads' lists is 696 tiles of 128, two rounds, the second short: 1.50 ms
     // whole, 1.42 in the two parts taken.
-    auto consider = [&](int tile) {
-        Plan p;
-        p.rows = tile;
-        p.tiles = (rows + tile - 1) / tile;
+    for (const TileCost& t : kTileCosts) {
+        // a tile more than half empty is never better; d = 64: three work-groups of
+        // 128 rows share a compute unit and one of 256 leaves a third of it empty
+        // (10,800 queries, 24 x 118,800 tokens 9.2 ms, 10.0 with 256 rows; d = 128,
+        // int8 16.2 with 256, 17.6 with 128)
+        if ((t.rows > 16 && t.rows >= 2 * rows) || (t.rows == 256 && (lists || d == 64))) continue;
+        CacheAttnPlan p{};
+        p.rows = t.rows;
+        p.tiles = (rows + t.rows - 1) / t.rows;
         p.heads = lists ? Hq : H;
-        p.units = B * p.heads * (lists ? (Lq + block - 1) / block : 1) * p.tiles;
-        const bool small = tile <= 32;
-        // resident work-groups; tokens of one turn of a work-group (a step of all
-        // its waves, a unit)
-        const int slots = small || tile == 256 ? 256 : d == 64 ? 768 : 512;
-        const int turn = small ? kStep * kRowWaves : kUnit;
-        const double walk = std::max(1.0, (lists ? 0.25 : 1.0) * max_len / turn);
-        const double exist = (double)std::min(tile, rows);
+        const long units = (long)B * p.heads * (lists ? (Lq + block - 1) / block : 1) * p.tiles;
+        const bool small = t.rows <= 32;
+        // resident work-groups; turns of a whole walk
+        const int slots = small || t.rows == 256 ? 256 : d == 64 ? 768 : 512;
+        const double walk = std::max(1.0, (lists ? 0.25 : 1.0) * max_len / (small ? kStep * kRowWaves : kUnit));
         auto weigh = [&](int c) {
-            const long items = (long)p.units * c;
-            if (c > 1 && items > (1L << 18)) return;   // (a launch's work-groups keep to their limit)
+            const long items = units * c;
+            // a launch's work-groups keep to their limit; the first tile, whole, does
+            if (least != 0.0 && items > (1L << 18)) return;
             const double rounds = (double)((items + slots - 1) / slots);
-            // a turn (the loads' latency, and the share of the bandwidth that the
-            // resident work-groups leave to one; or products and softmax), a start,
-            // a join (its launch, and the partial results at 4.5 TB/s both ways)
-            const double us = small ? 1.0 + 2.0 * turn * d * std::min<long>(items, slots) / 8.5e6
-                                    : tile == 256 ? 2.1 : (tile == 64 ? 0.6 : 1.0) * (items <= 256 ? 1.6 : 2.3);
-            const double start = small ? 3.0 : 8.0;
-            const double join = c == 1 ? 0.0 : 5.0 + 0.02 * c + 8.0 * items * exist * d / 4.5e6;
-            const double cost = rounds * (walk / c * us + start) + join;
+            const double us = (t.turn + t.more * (double)std::min<long>(items, slots) / 256) * (d == 64 ? t.half : 1.0);
+            const double join = c == 1 ? 0.0 : 3.1 + 0.023 * c + 1.2e-6 * items * std::min(t.rows, rows) * d;
+            const double cost = rounds * (walk / c * us + t.start) + join;
             if (least == 0.0 || cost < least) {
                 least = cost;
                 best = p;
+                best.units = (int)units;
                 best.C = c;
             }
         };
@@ -1045,23 +1056,16 @@ Plan plan_of(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool l
         const int most = std::min((int)walk, 256);
         for (int c = 1; c <= std::min(most, 8); ++c) weigh(c);
         for (int r = 1, c = 8; r <= 8 && c < most; ++r)
-            if (r * slots / p.units > 8) weigh(c = std::min(most, r * slots / p.units));
-    };
-    if (rows <= 16) consider(16);
-    else if (rows <= 32) consider(32);
-    else if (rows <= 64) consider(64);
-    else {
-        // d = 64: three work-groups of 128 rows share a compute unit and one of 256
-        // leaves a third of it empty (10,800 queries, 24 x 118,800 tokens 9.2 ms,
-        // 10.0 with 256 rows; d = 128, int8 16.2 with 256, 17.6 with 128)
-        consider(128);
-        if (!lists && rows > 128 && d == 128) consider(256);
+            if (r * slots / units > 8) weigh(c = (int)std::min<long>(most, r * slots / units));
     }
     return best;
 }
-size_t part_bytes(const Plan& p, int d) {
+
+size_t cache_attn_plan_bytes(const CacheAttnPlan& p, int d) {
     return p.C == 1 ? 0 : (size_t)p.units * p.C * p.rows * (d + 1) * sizeof(float);
 }
+
+namespace {
 
 template <int D, int FMT, int ROWS, bool LISTS>
 hipError_t launch(const AttnArgs& a, hipStream_t s) {
@@ -1085,16 +1089,10 @@ hipError_t launch(const AttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
-size_t cache_attn_ws_bytes(int B, int H, int d, int block, int Hq, int Lq, int max_len) {
-    return std::max(part_bytes(plan_of(B, H, d, block, Hq, Lq, max_len, false), d),
-                    part_bytes(plan_of(B, H, d, block, Hq, Lq, max_len, true), d));
-}
-
-hipError_t launch_cache_attn(const CacheView& c, const uint16_t* q, int Hq, int Lq, int max_len,
-                             const int32_t* kv_len, const int32_t* kv_idx, const int32_t* kv_cnt, float scale,
-                             uint16_t* o, float* lse, void* ws, hipStream_t s) {
+hipError_t launch_cache_attn(const CacheAttnPlan& p, const CacheView& c, const uint16_t* q, int Hq, int Lq,
+                             int max_len, const int32_t* kv_len, const int32_t* kv_idx, const int32_t* kv_cnt,
+                             float scale, uint16_t* o, float* lse, void* ws, hipStream_t s) {
     const bool lists = kv_idx != nullptr;
-    const Plan p = plan_of(c.B, c.H, c.d, c.block, Hq, Lq, max_len, lists);
     AttnArgs a{q, c.k, c.v, c.ks, c.vs, kv_len, kv_idx, kv_cnt, o, lse, static_cast<float*>(ws),
                c.B, Hq, c.H, Lq, c.cap, c.n, max_len, (max_len + c.block - 1) / c.block,
                (Lq + c.block - 1) / c.block, c.block, c.block == 128 ? 7 : 6, Hq / c.H, p.tiles, p.heads, p.C,

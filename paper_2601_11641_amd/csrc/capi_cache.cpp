@@ -108,6 +108,17 @@ mod_status check_attn(const mod_cache_shape* s, int Hq, int Lq, int max_len) {
     return MOD_OK;
 }
 
+// The plans without and with lists; the bytes that both can do with.
+size_t plan_attn(const mod_cache_shape* s, int Hq, int Lq, int max_len, moddit::CacheAttnPlan (&plans)[2]) {
+    size_t need = 0;
+    for (int lists = 0; lists < 2; ++lists) {
+        plans[lists] = moddit::plan_cache_attn(s->B, s->H, s->d, s->block, Hq, Lq, max_len, lists != 0);
+        const size_t bytes = moddit::cache_attn_plan_bytes(plans[lists], s->d);
+        if (bytes > need) need = bytes;
+    }
+    return need;
+}
+
 mod_status rope_call(const mod_rope* rope, const mod_shape* shape, const void* x, const mod_strides* xs, void* y,
                      const mod_strides* ys, int first, const int32_t* starts, bool backward, void* stream) {
     if (!rope) return fail(MOD_ERR_INVALID_ARG, "rope is NULL");
@@ -286,7 +297,8 @@ mod_status mod_cache_read(const mod_cache_shape* shape, const mod_cache* cache, 
 
 size_t mod_cache_attn_workspace_bytes(const mod_cache_shape* shape, int Hq, int Lq, int max_len) {
     if (check_attn(shape, Hq, Lq, max_len) != MOD_OK) return 0;
-    return moddit::cache_attn_ws_bytes(shape->B, shape->H, shape->d, shape->block, Hq, Lq, max_len);
+    moddit::CacheAttnPlan plans[2];
+    return plan_attn(shape, Hq, Lq, max_len, plans);
 }
 
 mod_status mod_cache_attn_fwd(const mod_cache_shape* shape, const mod_cache* cache, const void* q, int Hq, int Lq,
@@ -305,8 +317,8 @@ mod_status mod_cache_attn_fwd(const mod_cache_shape* shape, const mod_cache* cac
     if (!kv_idx != !kv_cnt) return fail(MOD_ERR_INVALID_ARG, "kv_idx and kv_cnt must both be given, or neither");
     if (!(scale >= 0.0f) || !std::isfinite(scale))
         return fail(MOD_ERR_INVALID_ARG, "scale must be finite and >= 0");
-    const size_t need =
-        moddit::cache_attn_ws_bytes(shape->B, shape->H, shape->d, shape->block, Hq, Lq, max_len);
+    moddit::CacheAttnPlan plans[2];
+    const size_t need = plan_attn(shape, Hq, Lq, max_len, plans);
     if (need > 0) {
         if (!workspace || ws_bytes < need)
             return fail(MOD_ERR_INVALID_ARG, "workspace of at least %zu bytes needed (got %zu%s)", need, ws_bytes,
@@ -315,8 +327,9 @@ mod_status mod_cache_attn_fwd(const mod_cache_shape* shape, const mod_cache* cac
         if (st != MOD_OK) return st;
     }
     const float sc = scale == 0.0f ? (float)(1.0 / std::sqrt((double)shape->d)) : scale;
-    const hipError_t e = moddit::launch_cache_attn(view, static_cast<const uint16_t*>(q), Hq, Lq, max_len, kv_len,
-                                                   kv_idx, kv_cnt, sc, static_cast<uint16_t*>(o), lse, workspace,
+    const hipError_t e = moddit::launch_cache_attn(plans[kv_idx != nullptr], view, static_cast<const uint16_t*>(q),
+                                                   Hq, Lq, max_len, kv_len, kv_idx, kv_cnt, sc,
+                                                   static_cast<uint16_t*>(o), lse, workspace,
                                                    static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "cache attention launch");
     return MOD_OK;

@@ -119,10 +119,17 @@ hipError_t launch_cache_write(const CacheView& c, const Strided& k, const Stride
 hipError_t launch_cache_read(const CacheView& c, const Strided& k, const Strided& v, int L, int first,
                              const int32_t* starts, const int32_t* counts, hipStream_t s);
 
-// Attention over the cache.  ws: at least cache_attn_ws_bytes.
-size_t cache_attn_ws_bytes(int B, int H, int d, int block, int Hq, int Lq, int max_len);
-hipError_t launch_cache_attn(const CacheView& c, const uint16_t* q, int Hq, int Lq, int max_len,
-                             const int32_t* kv_len, const int32_t* kv_idx, const int32_t* kv_cnt, float scale,
-                             uint16_t* o, float* lse, void* ws, hipStream_t s);
+// Attention over the cache: how a call is cut up, from its host sizes alone, the
+// workspace that takes, and its launch (ws: at least so many bytes).
+struct CacheAttnPlan {
+    int rows;                  // rows of a tile: 16, 32 (rows_kernel), 64, 128, 256 (tile_kernel)
+    int C;                     // parts of a walk
+    int tiles, heads, units;   // as in the kernels' arguments
+};
+CacheAttnPlan plan_cache_attn(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool lists);
+size_t cache_attn_plan_bytes(const CacheAttnPlan& p, int d);
+hipError_t launch_cache_attn(const CacheAttnPlan& p, const CacheView& c, const uint16_t* q, int Hq, int Lq,
+                             int max_len, const int32_t* kv_len, const int32_t* kv_idx, const int32_t* kv_cnt,
+                             float scale, uint16_t* o, float* lse, void* ws, hipStream_t s);
 
 }  // namespace moddit

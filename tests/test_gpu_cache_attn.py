@@ -76,8 +76,10 @@ class Filled:
         return o, lse
 
 
-def check(f, q, o, lse, lens, scale, kept=None):
+def check(f, q, o, lse, lens, scale, kept=None, lost=None):
+    """lost: what fp32 does not hold of an output."""
     want, wl, eo, el = R.attention(q, *f.kv, lens, f.block, scale, kept)
+    eo = eo if lost is None else eo + lost
     o, lse = o.cpu().double(), lse.cpu().double()
     assert torch.equal(lse == -math.inf, wl == -math.inf)
     none = wl == -math.inf
@@ -433,3 +435,116 @@ def test_strided_views_and_shared_tensors(M):
     for q, o in ((bad, outs[0]), (qd[0], bad)):
         with pytest.raises(ValueError):
             M.mod_cache_attn_fwd(f.shape, f.ref, q, 5000, ld, None, None, 0.0, o)
+
+
+# Calls large enough for tiles of 256 (d = 128 without lists), 128, 64 and 32 rows,
+# each whole and in parts where it is chosen so: d, block, B, H, query heads per
+# head, Lq, tokens, lists
+MANY_ROWS = [
+    (128, 64, 3, 16, 2, 129, 700, False), (128, 128, 2, 16, 1, 129, 1500, False),     # 256
+    (128, 128, 2, 16, 1, 70, 70, False), (128, 64, 1, 1, 1, 70, 700, False),           # 128
+    (64, 64, 2, 16, 2, 129, 70, False), (64, 128, 3, 2, 2, 700, 500, False),
+    (128, 128, 3, 1, 2, 129, 70, True), (128, 128, 1, 1, 1, 70, 3000, True),
+    (64, 128, 3, 8, 2, 129, 70, True), (64, 128, 3, 16, 2, 70, 2000, True),
+    (128, 128, 3, 16, 1, 40, 3000, False),                                             # 64
+    (64, 128, 2, 16, 2, 300, 700, False), (64, 64, 3, 16, 2, 129, 2000, False),
+    (128, 64, 3, 8, 2, 129, 70, True), (128, 64, 3, 8, 2, 129, 3000, True),
+    (64, 64, 3, 8, 2, 129, 70, True), (64, 128, 3, 16, 2, 129, 3000, True),
+    (128, 64, 1, 16, 2, 129, 130, False), (128, 128, 1, 8, 1, 40, 4000, False),        # 32
+    (64, 64, 1, 16, 2, 129, 70, False), (64, 128, 1, 1, 1, 700, 2000, False),
+    (128, 64, 3, 2, 2, 70, 4000, True), (64, 64, 3, 4, 2, 129, 70, True),
+]
+
+
+def flushed(f, group):
+    """What fp32 does not hold of an output: a probability p (of a row's largest)
+    and its product with the value scale s are 0 under 2^-126, so a token of code
+    c may lose p |c s| <= 2^-126 |c| max(1, s)."""
+    codes, scales = R.numbers(f.codes[1], f.fmt).abs(), f.scales[1].double()
+    lost = torch.zeros(f.B, f.H, 1, f.d, dtype=torch.float64)
+    for b in range(f.B):
+        at = torch.arange(f.lens[b])
+        lost[b, :, 0] = (codes[b, :, at] * scales[b, :, at // f.block, None].clamp(min=1.0)).sum(1)
+    return 2.0 ** -126 * lost.repeat_interleave(group, 1)
+
+
+@pytest.mark.parametrize("fmt", [R.E4M3, R.INT8])
+@pytest.mark.parametrize("case", MANY_ROWS)
+def test_many_rows(M, case, fmt):
+    """Scores that make the running maximum move, sequences of different lengths
+    (none among them), and in head 0 value scales from 2^-100 to 2^100 and zero
+    side by side, and a key scale of zero."""
+    d, block, B, H, group, Lq, L, lists = case
+    lens = [L, max(1, L // 3 - 5), 0][:B]
+    f = Filled(M, B, H, L, d, block, fmt, lens, seed=Lq + L, spread=3.0)
+    for t, vals in ((1, [2.0 ** -100, 1.0, 0.0, 2.0 ** 66, 2.0 ** -66, 3.0, 2.0 ** 100, 0.0, 2.0 ** -3]),
+                    (0, [None] * 4 + [0.0] * 2)):
+        for b in range(B):
+            for j, x in enumerate(vals[:-(-lens[b] // block)]):
+                if x is not None:
+                    f.scales[t][b, 0, j] = x
+    f.dev[2].copy_(f.scales[0])
+    f.dev[3].copy_(f.scales[1])
+    f.kv = tuple(R.dequant_by(c, s, fmt, block) for c, s in zip(f.codes, f.scales))
+    q = queries(B, H * group, Lq, d, Lq, 2.0)
+    idx = cnt = kept = None
+    if lists:
+        idx, cnt, kept = f.lists(H * group, -(-Lq // block), L, L, 0.6)
+    args = (q, L, torch.tensor(lens, dtype=torch.int32), idx, cnt)
+    o, lse = f.run(*args)
+    check(f, q, o, lse, lens, d ** -0.5, kept, flushed(f, group))
+    again = f.run(*args)
+    assert torch.equal(again[0], o) and torch.equal(again[1], lse)
+
+
+@pytest.mark.parametrize("case", [c for c in MANY_ROWS if c[2] > 1])
+def test_many_rows_with_large_scores_and_short_sequences(M, case):
+    """Scores up to a few hundred, and sequences much shorter than the cut-up
+    length, which leave parts without a token."""
+    d, block, B, H, group, Lq, L, lists = case
+    lens = [min(L, 40), L, 1][:B]
+    f = Filled(M, B, H, L, d, block, R.INT8, lens, seed=3, spread=12.0)
+    q = queries(B, H * group, Lq, d, 5, 3.0)
+    idx = cnt = kept = None
+    if lists:
+        idx, cnt, kept = f.lists(H * group, -(-Lq // block), L, L, 0.6)
+    o, lse = f.run(q, L, torch.tensor(lens, dtype=torch.int32), idx, cnt)
+    check(f, q, o, lse, lens, d ** -0.5, kept, flushed(f, group))
+
+
+@pytest.mark.parametrize("case", MANY_ROWS)
+def test_many_rows_with_infinities_and_nan(M, case):
+    """An infinite query gives NaN in its own row alone; a NaN scale in the rows
+    of the head that read its block and in no others."""
+    d, block, B, H, group, Lq, L, lists = case
+    f = Filled(M, B, H, L, d, block, R.E4M3, [L] * B)
+    q = queries(B, H * group, Lq, d, 1)
+    n, nq = -(-L // block), -(-Lq // block)
+    idx = cnt = None
+    if lists:      # every query block but the first lists all blocks, that one all but block 0
+        idx = torch.arange(n, dtype=torch.int32).expand(B, H * group, nq, n).contiguous()
+        cnt = torch.full((B, H * group, nq), n, dtype=torch.int32)
+        idx[:, :, 0] = idx[:, :, 0].flip(-1)
+        cnt[:, :, 0] = n - 1
+    o0, lse0 = f.run(q, L, None, idx, cnt)
+    row = Lq - 1
+    q2 = q.clone()
+    q2[B - 1, 0, row, 3] = math.inf
+    o, lse = f.run(q2, L, None, idx, cnt)
+    some = cnt is None or cnt[0, 0, row // block] > 0
+    if some:
+        assert not o[B - 1, 0, row].isfinite().any() and not lse[B - 1, 0, row].isfinite()
+    o[B - 1, 0, row], lse[B - 1, 0, row] = o0[B - 1, 0, row], lse0[B - 1, 0, row]
+    assert torch.equal(o, o0) and torch.equal(lse, lse0)
+    for t in (2, 3):
+        f.dev[t].copy_(f.scales[t - 2])
+        f.dev[t][B - 1, H - 1, 0] = math.nan
+        o, lse = f.run(q, L, None, idx, cnt)
+        hit = torch.zeros(B, H * group, Lq, dtype=torch.bool)
+        hit[B - 1, (H - 1) * group:] = True
+        if lists:
+            hit[:, :, :block] = False
+        hit = hit.cuda()
+        assert o[hit].isnan().all() and torch.equal(o[~hit], o0[~hit]) and torch.equal(lse[~hit], lse0[~hit])
+        assert lse[hit].isnan().all() if t == 2 else torch.all((lse[hit] - lse0[hit]).abs() <= 1e-5)
+        f.dev[t].copy_(f.scales[t - 2])
