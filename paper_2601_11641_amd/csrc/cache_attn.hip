@@ -996,16 +996,16 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
 // each work-group per compute unit adds to it, its start and end, and how much of
 // a turn d = 64 takes.  A fit to 11,000 calls with 1 to 16,384 queries, 64 to
 // 185,000 tokens, with and without lists, each with up to 60 ways to cut it up:
-// the way chosen by it is 2 to 3% slower than the best one measured, on average.
+// the way chosen by it is 2% slower than the best one measured, on average.
 struct TileCost {
     int rows;
     double turn, more, start, half;
 };
-constexpr TileCost kTileCosts[] = {{256, 1.4, 0.2, 7.0, 1.0},
-                                   {128, 1.4, 0.3, 6.0, 0.77},
-                                   {64, 1.2, 0.15, 9.0, 0.66},
-                                   {32, 2.5, 0.0, 6.0, 0.4},
-                                   {16, 2.2, 0.6, 5.0, 0.54}};
+constexpr TileCost kTileCosts[] = {{256, 1.5, 0.26, 8.5, 1.0},
+                                   {128, 1.45, 0.4, 7.3, 0.76},
+                                   {64, 1.25, 0.16, 11.0, 0.71},
+                                   {32, 2.35, 0.0, 7.0, 0.5},
+                                   {16, 2.0, 0.55, 4.0, 0.6}};
 
 }  // namespace
 
@@ -1032,7 +1032,8 @@ CacheAttnPlan plan_cache_attn(int B, int H, int d, int block, int Hq, int Lq, in
         p.rows = t.rows;
         p.tiles = (rows + t.rows - 1) / t.rows;
         p.heads = lists ? Hq : H;
-        const long units = (long)B * p.heads * (lists ? (Lq + block - 1) / block : 1) * p.tiles;
+        const long blocks = lists ? (Lq + block - 1) / block : 1, units = B * p.heads * blocks * p.tiles;
+        p.stretch = (int)((blocks * p.tiles + kXcds - 1) / kXcds);
         const bool small = t.rows <= 32;
         // resident work-groups; turns of a whole walk
         const int slots = small || t.rows == 256 ? 256 : d == 64 ? 768 : 512;
@@ -1041,9 +1042,11 @@ CacheAttnPlan plan_cache_attn(int B, int H, int d, int block, int Hq, int Lq, in
             const long items = units * c;
             // a launch's work-groups keep to their limit; the first tile, whole, does
             if (least != 0.0 && items > (1L << 18)) return;
-            const double rounds = (double)((items + slots - 1) / slots);
+            // of the die that gets the most
+            const long share = (items + kXcds * p.stretch - 1) / (kXcds * p.stretch) * p.stretch;
+            const double rounds = (double)((share + slots / kXcds - 1) / (slots / kXcds));
             const double us = (t.turn + t.more * (double)std::min<long>(items, slots) / 256) * (d == 64 ? t.half : 1.0);
-            const double join = c == 1 ? 0.0 : 3.1 + 0.023 * c + 1.2e-6 * items * std::min(t.rows, rows) * d;
+            const double join = c == 1 ? 0.0 : 5.0 + 0.02 * c + 1.3e-6 * items * std::min(t.rows, rows) * d;
             const double cost = rounds * (walk / c * us + t.start) + join;
             if (least == 0.0 || cost < least) {
                 least = cost;
@@ -1096,7 +1099,7 @@ hipError_t launch_cache_attn(const CacheAttnPlan& p, const CacheView& c, const u
     AttnArgs a{q, c.k, c.v, c.ks, c.vs, kv_len, kv_idx, kv_cnt, o, lse, static_cast<float*>(ws),
                c.B, Hq, c.H, Lq, c.cap, c.n, max_len, (max_len + c.block - 1) / c.block,
                (Lq + c.block - 1) / c.block, c.block, c.block == 128 ? 7 : 6, Hq / c.H, p.tiles, p.heads, p.C,
-               ((lists ? (Lq + c.block - 1) / c.block : 1) * p.tiles + kXcds - 1) / kXcds, p.units, scale * kLog2e};
+               p.stretch, p.units, scale * kLog2e};
     hipError_t e = hipErrorInvalidValue;
     auto with_rt = [&](auto d, auto fmt, auto ls) {
         constexpr int D = decltype(d)::value, FMT = decltype(fmt)::value;

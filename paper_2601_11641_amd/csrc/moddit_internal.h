@@ -124,7 +124,7 @@ hipError_t launch_cache_read(const CacheView& c, const Strided& k, const Strided
 struct CacheAttnPlan {
     int rows;                  // rows of a tile: 16, 32 (rows_kernel), 64, 128, 256 (tile_kernel)
     int C;                     // parts of a walk
-    int tiles, heads, units;   // as in the kernels' arguments
+    int tiles, heads, units, stretch;   // as in the kernels' arguments
 };
 CacheAttnPlan plan_cache_attn(int B, int H, int d, int block, int Hq, int Lq, int max_len, bool lists);
 size_t cache_attn_plan_bytes(const CacheAttnPlan& p, int d);

@@ -437,22 +437,22 @@ def test_strided_views_and_shared_tensors(M):
             M.mod_cache_attn_fwd(f.shape, f.ref, q, 5000, ld, None, None, 0.0, o)
 
 
-# Calls large enough for tiles of 256 (d = 128 without lists), 128, 64 and 32 rows,
-# each whole and in parts where it is chosen so: d, block, B, H, query heads per
+# Calls that take tiles of 256 (d = 128 without lists), 128, 64, 32 and 16 rows, each
+# whole and in parts where it is chosen so: d, block, B, H, query heads per
 # head, Lq, tokens, lists
 MANY_ROWS = [
-    (128, 64, 3, 16, 2, 129, 700, False), (128, 128, 2, 16, 1, 129, 1500, False),     # 256
-    (128, 128, 2, 16, 1, 70, 70, False), (128, 64, 1, 1, 1, 70, 700, False),           # 128
-    (64, 64, 2, 16, 2, 129, 70, False), (64, 128, 3, 2, 2, 700, 500, False),
-    (128, 128, 3, 1, 2, 129, 70, True), (128, 128, 1, 1, 1, 70, 3000, True),
-    (64, 128, 3, 8, 2, 129, 70, True), (64, 128, 3, 16, 2, 70, 2000, True),
-    (128, 128, 3, 16, 1, 40, 3000, False),                                             # 64
-    (64, 128, 2, 16, 2, 300, 700, False), (64, 64, 3, 16, 2, 129, 2000, False),
-    (128, 64, 3, 8, 2, 129, 70, True), (128, 64, 3, 8, 2, 129, 3000, True),
-    (64, 64, 3, 8, 2, 129, 70, True), (64, 128, 3, 16, 2, 129, 3000, True),
-    (128, 64, 1, 16, 2, 129, 130, False), (128, 128, 1, 8, 1, 40, 4000, False),        # 32
-    (64, 64, 1, 16, 2, 129, 70, False), (64, 128, 1, 1, 1, 700, 2000, False),
-    (128, 64, 3, 2, 2, 70, 4000, True), (64, 64, 3, 4, 2, 129, 70, True),
+    (128, 128, 2, 16, 1, 129, 5000, False), (128, 64, 3, 24, 1, 700, 500, False),      # 256
+    (128, 128, 3, 24, 1, 100, 70, False), (128, 64, 2, 16, 1, 70, 5000, False),        # 128
+    (64, 64, 2, 16, 2, 129, 70, False), (64, 128, 3, 16, 1, 70, 9000, False),
+    (128, 128, 3, 12, 1, 129, 70, True), (128, 128, 3, 16, 2, 70, 5000, True),
+    (64, 128, 3, 12, 1, 129, 70, True), (64, 128, 3, 16, 2, 70, 9000, True),
+    (128, 128, 3, 16, 2, 17, 9000, False), (64, 64, 3, 24, 1, 33, 9000, False),        # 64
+    (128, 64, 3, 12, 2, 70, 70, True), (128, 64, 3, 12, 2, 70, 5000, True),
+    (64, 64, 3, 12, 2, 70, 70, True), (64, 64, 3, 12, 2, 70, 9000, True),
+    (128, 64, 2, 8, 2, 129, 300, False), (128, 128, 3, 16, 1, 17, 3000, False),        # 32
+    (64, 64, 2, 8, 2, 129, 300, False), (64, 128, 3, 12, 1, 17, 5000, False),
+    (128, 64, 3, 12, 2, 17, 9000, True), (64, 64, 3, 12, 1, 70, 70, True), (64, 128, 3, 16, 2, 40, 70, True),
+    (128, 64, 2, 1, 1, 17, 1000, False), (64, 128, 2, 1, 1, 17, 9000, True),           # 16, two tiles
 ]
 
 
