@@ -1021,7 +1021,7 @@ CacheAttnPlan plan_cache_attn(int B, int H, int d, int block, int Hq, int Lq, in
     // 32 parts (taken).  1024 queries over 8 heads of 1024: 18 us in tiles of 32
     // (taken), 23 in tiles of 128 and three parts.  One frame of 3600 queries over
     // 24 heads' lists is 696 tiles of 128, two rounds, the second short: 1.50 ms
-    // whole, 1.42 in the two parts taken.
+    // whole, 1.42 in two parts, 1.40 in five (taken).
     for (const TileCost& t : kTileCosts) {
         // a tile more than half empty is never better; d = 64: three work-groups of
         // 128 rows share a compute unit and one of 256 leaves a third of it empty
@@ -1040,14 +1040,16 @@ CacheAttnPlan plan_cache_attn(int B, int H, int d, int block, int Hq, int Lq, in
         const double walk = std::max(1.0, (lists ? 0.25 : 1.0) * max_len / (small ? kStep * kRowWaves : kUnit));
         auto weigh = [&](int c) {
             const long items = units * c;
-            // a launch's work-groups keep to their limit; the first tile, whole, does
-            if (least != 0.0 && items > (1L << 18)) return;
+            // past 64 rounds parts save nothing; a launch's work-groups keep to their
+            // limit, as those of the first tile, whole, do
+            if (least != 0.0 && items > (c > 1 ? 1L << 14 : 1L << 18)) return;
             // of the die that gets the most
             const long share = (items + kXcds * p.stretch - 1) / (kXcds * p.stretch) * p.stretch;
             const double rounds = (double)((share + slots / kXcds - 1) / (slots / kXcds));
             const double us = (t.turn + t.more * (double)std::min<long>(items, slots) / 256) * (d == 64 ? t.half : 1.0);
             const double join = c == 1 ? 0.0 : 5.0 + 0.02 * c + 1.3e-6 * items * std::min(t.rows, rows) * d;
-            const double cost = rounds * (walk / c * us + t.start) + join;
+            // (parts, and the memory they take, have to save 1%)
+            const double cost = (rounds * (walk / c * us + t.start) + join) * (c == 1 ? 1.0 : 1.01);
             if (least == 0.0 || cost < least) {
                 least = cost;
                 best = p;
