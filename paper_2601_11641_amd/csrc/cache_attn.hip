@@ -136,6 +136,17 @@ __device__ __forceinline__ float sum4(float x) {
     return x + __shfl_xor(x, 32);
 }
 
+// A value that all lanes share, in a scalar register.
+__device__ __forceinline__ float uniform(float x) {
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
+
+// Value scales under 2^-64 (a write gives 2^-126 on): their products with
+// probabilities below one may be subnormal bf16, of fewer bits.  They enter
+// 2^64 times as large, and 2^-64 elsewhere: exact.
+__device__ __forceinline__ bool small_scale(float s) { return s > 0.0f && s < 0x1p-64f; }
+constexpr uint32_t kSmallScale = 0x1f800000u;   // 2^-64: the bits of positive numbers have their order
+
 __device__ __forceinline__ int clamp_len(const AttnArgs& a, int b) {
     return a.len ? min(max(a.len[b], 0), a.max_len) : a.max_len;
 }
@@ -263,9 +274,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void rows_kernel(AttnArgs a) {
     };
     // two steps are under way: the codes of the next arrive while one is computed
     Step even, odd;
-    int s = s0 + wave;
-    load(even, s, entry_of(s));
-    int jn = entry_of(s + WAVES);
+    load(even, s0 + wave, entry_of(s0 + wave));
 
     // Q as the second operand: row l16 of tile rt, the channels that a lane of
     // group g loads of K
@@ -283,18 +292,17 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void rows_kernel(AttnArgs a) {
     }
     f32x4 acc[RT][VF];
     float m[RT], l[RT];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        m[rt] = -INFINITY;
-        l[rt] = 0.0f;
-#pragma unroll
-        for (int f = 0; f < VF; ++f) acc[rt][f] = f32x4{0, 0, 0, 0};
-    }
+    uint32_t least = ~0u;               // bits of the smallest value scale but zero, less one
 
-    auto compute = [&](const Step& y) __attribute__((always_inline)) {
+    // SMALL: value scales of any size (see small_scale)
+    auto compute = [&](const Step& y, auto small_tag) __attribute__((always_inline)) {
+        constexpr bool SMALL = decltype(small_tag)::value;
         const int t0 = __builtin_amdgcn_readfirstlane(y.t0);
         if (t0 < 0) return;
         const float sc = y.ks * a.c2;
+        const bool up = SMALL && small_scale(y.vs);
+        const float vs = up ? y.vs * 0x1p64f : y.vs, down = up ? 0x1p-64f : 1.0f;
+        if constexpr (!SMALL) least = min(least, (uint32_t)__builtin_amdgcn_readfirstlane(__float_as_uint(y.vs)) - 1);
         f32x4 st[RT][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -333,8 +341,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void rows_kernel(AttnArgs a) {
             for (int e = 0; e < 8; ++e) {
                 const float p = __builtin_amdgcn_exp2f(x[e] - mb);
                 l[rt] += p;
-                pf[rt][e] = static_cast<__bf16>(p * y.vs);
-                if constexpr (TWICE) pl[rt][e] = static_cast<__bf16>(p * y.vs - static_cast<float>(pf[rt][e]));
+                pf[rt][e] = static_cast<__bf16>(p * vs);
+                if constexpr (TWICE) pl[rt][e] = static_cast<__bf16>(p * vs - static_cast<float>(pf[rt][e]));
             }
         }
         static_for<VF>([&](auto f_tag) __attribute__((always_inline)) {
@@ -344,19 +352,37 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void rows_kernel(AttnArgs a) {
             const bf16x8 vf = __builtin_bit_cast(bf16x8, x);
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                acc[rt][F] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rt], acc[rt][F], 0, 0, 0);
-                if constexpr (TWICE) acc[rt][F] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[rt], acc[rt][F], 0, 0, 0);
+                f32x4 sum = SMALL ? f32x4{0, 0, 0, 0} : acc[rt][F];
+                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rt], sum, 0, 0, 0);
+                if constexpr (TWICE) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pl[rt], sum, 0, 0, 0);
+                acc[rt][F] = SMALL ? acc[rt][F] + sum * down : sum;
             }
         });
     };
-    while (s < s1) {
-        load(odd, s + WAVES, jn);
-        jn = entry_of(s + 2 * WAVES);
-        compute(even);
-        s += 2 * WAVES;
-        load(even, s, jn);
-        jn = entry_of(s + WAVES);
-        compute(odd);
+    // the wave's steps, the first one's codes under way
+    auto walk = [&](auto small_tag) __attribute__((always_inline)) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            m[rt] = -INFINITY;
+            l[rt] = 0.0f;
+#pragma unroll
+            for (int f = 0; f < VF; ++f) acc[rt][f] = f32x4{0, 0, 0, 0};
+        }
+        int s = s0 + wave, jn = entry_of(s + WAVES);
+        while (s < s1) {
+            load(odd, s + WAVES, jn);
+            jn = entry_of(s + 2 * WAVES);
+            compute(even, small_tag);
+            s += 2 * WAVES;
+            load(even, s, jn);
+            jn = entry_of(s + WAVES);
+            compute(odd, small_tag);
+        }
+    };
+    walk(std::false_type{});
+    if (least < kSmallScale - 1) {      // rare: once more
+        load(even, s0 + wave, entry_of(s0 + wave));
+        walk(std::true_type{});
     }
 
     // join the waves
@@ -453,17 +479,20 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void rows_kernel(AttnArgs a) {
 // ---------------------------------------------------------------------------
 constexpr int kUnit = 64;
 
-// A value that all lanes share, in a scalar register.
-__device__ __forceinline__ float uniform(float x) {
-    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
-}
-
 // What the softmax needs to know of a unit.
 struct Unit {
     float sc;       // scale * s_k, in units of log 2
-    float lv, ivs;  // log2 s_v and 1 / s_v (0 and 1 where the scale goes into the values instead)
+    float lv, ivs;  // log2 s and 1 / s of the value scale's part s that stands in the exponent
     int valid;      // tokens of the unit that exist
 };
+
+// The part of a value scale that goes into the values: 1, or a power of two
+// that leaves between 2^-64 and 2^64 for the exponent (so the values stay exact
+// and the probabilities normal), or 0 and NaN themselves.  For scales outside that
+// range:
+__device__ __forceinline__ float value_part(float s) {
+    return small_scale(s) ? 0x1p-64f : s > 0x1p64f && s < INFINITY ? 0x1p64f : s;
+}
 
 template <int D, int FMT, bool LISTS, int ROWS>
 __global__ __launch_bounds__(64 * kTileWaves<ROWS>, 2) void tile_kernel(AttnArgs a) {
@@ -588,7 +617,7 @@ __global__ __launch_bounds__(64 * kTileWaves<ROWS>, 2) void tile_kernel(AttnArgs
                 make_uint4(conv[0], conv[1], conv[2], conv[3]);
     };
     constexpr int PAIRS = CPT / 2;               // pairs of codes per thread and tile
-    // V whose scale cannot stand in the exponent (0, NaN, extreme): into the values
+    // V times the part of its scale that goes into the values
     auto stage_scaled = [&](char* to, float s) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NP; ++i)
@@ -752,10 +781,16 @@ __global__ __launch_bounds__(64 * kTileWaves<ROWS>, 2) void tile_kernel(AttnArgs
             }
         }
     };
-    auto unit_of = [&](int t0, float ks, float vs) __attribute__((always_inline)) {
-        const bool plain = vs >= 0x1p-64f && vs <= 0x1p64f;
-        return Unit{uniform(ks * a.c2), uniform(plain ? __builtin_amdgcn_logf(vs) : 0.0f),
-                    uniform(plain ? __builtin_amdgcn_rcpf(vs) : 1.0f), t0 < 0 ? 0 : len - t0};
+    // a unit's scales; of the value scale `vs` only what goes into the values is left
+    auto unit_of = [&](int t0, float ks, float& vs) __attribute__((always_inline)) {
+        float in_p = uniform(vs);
+        vs = 1.0f;
+        if (!(in_p >= 0x1p-64f && in_p <= 0x1p64f)) {
+            vs = uniform(value_part(in_p));
+            in_p = uniform(vs == 0x1p-64f ? in_p * 0x1p64f : vs == 0x1p64f ? in_p * 0x1p-64f : 1.0f);
+        }
+        return Unit{uniform(ks * a.c2), uniform(__builtin_amdgcn_logf(in_p)), uniform(__builtin_amdgcn_rcpf(in_p)),
+                    t0 < 0 ? 0 : len - t0};
     };
     // first tokens of this unit and the next, list entry of the one after
     int tc = -1, tn = -1, jn = 0;
@@ -780,13 +815,13 @@ __global__ __launch_bounds__(64 * kTileWaves<ROWS>, 2) void tile_kernel(AttnArgs
             if (t + 3 < T) jn = entry_of(t + 3);
         }
         half(I1{}, ka + 32 * KROW, va + 32 * VROW, Yes{}, Yes{}, Rest{}, No{}, Yes{}, No{}, now, kst, vto, 0, 0);
-        if (!(vs >= 0x1p-64f && vs <= 0x1p64f)) stage_scaled(vto, vs);
+        if (vs != 1.0f) stage_scaled(vto, vs);
         if (t + 1 < T) load(vcodes, tn, vr);
         barrier();
         read_ahead(kad + kn, vad + vc);
         before = now;
         now = unit_of(tn, ksn, vsn);
-        vs = uniform(vsn);
+        vs = vsn;
         tn = tnn;
         kc = kn;
         vp = vc;
@@ -803,7 +838,7 @@ __global__ __launch_bounds__(64 * kTileWaves<ROWS>, 2) void tile_kernel(AttnArgs
             fetch_scales(tn, ksn, vsn);
             half(sub_tag, kad + SUB * KTILE, vad + SUB * VTILE, Yes{}, Yes{}, Yes{}, Yes{}, Yes{}, No{}, before,
                  kst + OTHER * KTILE, vto, 0, 0);
-            if (!(vs >= 0x1p-64f && vs <= 0x1p64f)) stage_scaled(vto, vs);
+            if (vs != 1.0f) stage_scaled(vto, vs);
             load(vcodes, tc, vr);
             int tnn = -1;
             if (j + 2 < T) {
@@ -816,7 +851,7 @@ __global__ __launch_bounds__(64 * kTileWaves<ROWS>, 2) void tile_kernel(AttnArgs
             before = now;
             vs = vnow;
             now = unit_of(tn, ksn, vsn);
-            vnow = uniform(vsn);
+            vnow = vsn;
             tc = tn;
             tn = tnn;
         };
@@ -830,7 +865,6 @@ __global__ __launch_bounds__(64 * kTileWaves<ROWS>, 2) void tile_kernel(AttnArgs
             load(kcodes, tc, kr);
             fetch_scales(tc, ks, vnow);
             now = unit_of(tc, ks, vnow);
-            vnow = uniform(vnow);
             before = Unit{0.0f, 0.0f, 1.0f, 0};
             static_for<PAIRS>([&](auto q) __attribute__((always_inline)) { convert(q, KR{}, kr, kst, kconv); });
             if (T > 1) {
@@ -872,7 +906,6 @@ __global__ __launch_bounds__(64 * kTileWaves<ROWS>, 2) void tile_kernel(AttnArgs
         load(kcodes, tc, kr);
         fetch_scales(tc, ks, vs);
         now = unit_of(tc, ks, vs);
-        vs = uniform(vs);
         static_for<PAIRS>([&](auto q) __attribute__((always_inline)) { convert(q, KR{}, kr, kst, kconv); });
         if (T > 1) {
             tn = token_of(1, entry_of(1));

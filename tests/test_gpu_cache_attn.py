@@ -548,3 +548,59 @@ def test_many_rows_with_infinities_and_nan(M, case):
         assert o[hit].isnan().all() and torch.equal(o[~hit], o0[~hit]) and torch.equal(lse[~hit], lse0[~hit])
         assert lse[hit].isnan().all() if t == 2 else torch.all((lse[hit] - lse0[hit]).abs() <= 1e-5)
         f.dev[t].copy_(f.scales[t - 2])
+
+
+# value scales from the smallest that a write gives on, past 2^-64 and 2^64 on
+# either side
+FAR = [2.0 ** -126, 1.37 * 2.0 ** -126, 1.9 * 2.0 ** -125, 1.37 * 2.0 ** -100, 1.9 * 2.0 ** -65, 1.37 * 2.0 ** 66,
+       1.37 * 2.0 ** 110]
+
+
+@pytest.mark.parametrize("fmt", [R.E4M3, R.INT8])
+@pytest.mark.parametrize("sv", FAR)
+@pytest.mark.parametrize("Lq,lists", [(1, False), (20, False), (150, False), (2000, False), (20, True), (150, True)])
+def test_value_scales_of_the_whole_range(M, fmt, sv, Lq, lists):
+    """Probabilities below one times the smallest scales: nothing is lost but
+    what fp32 sums (at most four roundings a token, 2^-150 each) and the bf16
+    output (half a step of 2^-133) do not hold."""
+    if fmt == R.E4M3:
+        sv = 2.0 ** math.floor(math.log2(sv))
+    d, block, n, H = 128, 128, 5, 16
+    f = Filled(M, 1, H, n * block, d, block, fmt, [n * block], seed=8)
+    f.scales[1].fill_(sv)
+    f.dev[3].copy_(f.scales[1])
+    f.kv = tuple(R.dequant_by(c, s, fmt, block) for c, s in zip(f.codes, f.scales))
+    q = queries(1, H, Lq, d, 3)
+    idx = cnt = kept = None
+    if lists:
+        idx, cnt, kept = f.lists(H, -(-Lq // block), n * block, Lq, 0.7)
+    o, lse = f.run(q, n * block, None, idx, cnt)
+    check(f, q, o, lse, [n * block], d ** -0.5, kept, 2.0 ** -134 + 4 * n * block * 2.0 ** -150)
+
+
+@pytest.mark.parametrize("sv", FAR)
+@pytest.mark.parametrize("case", MANY_ROWS)
+def test_codes_stay_exact_under_any_scale(M, case, sv):
+    """Equal scores give every token of a sequence the same rounded probability,
+    a common factor of the output, so values that nearly cancel leave errors of
+    the small sum and not of its terms: two half steps of bf16 of the output and
+    the roundings of fp32 sums (at most four per token of the sum of magnitudes;
+    2^-150 each where that is subnormal)."""
+    d, block, B, H, group, Lq, L, lists = case
+    f = Filled(M, B, H, L, d, block, R.INT8, [L] * B)
+    c = 60 + torch.arange(d) % 64
+    codes = torch.where((torch.arange(L) % 2 == 0)[:, None], c, 1 - c).to(torch.int8)
+    f.dev[1].copy_(codes.view(torch.uint8).expand(B, H, L, d))
+    f.dev[3].fill_(sv)
+    sv = float(f.dev[3][0, 0, 0])
+    idx = cnt = None
+    n, nq = -(-L // block), -(-Lq // block)
+    if lists:
+        idx = torch.arange(n, dtype=torch.int32).expand(B, H * group, nq, n).contiguous()
+        cnt = torch.full((B, H * group, nq), n, dtype=torch.int32)
+    o, lse = f.run(torch.zeros((B, H * group, Lq, d), dtype=torch.bfloat16), L, None, idx, cnt)
+    want, size = codes.double().mean(0) * sv, codes.double().abs().mean(0) * sv
+    bound = 2.01 * R.BF16 * want.abs() + 4 * L * (R.F32 * size + 2.0 ** -150) + 2.0 ** -134
+    off = (o.cpu().double() - want).abs()
+    assert torch.all(off <= bound), (off / bound).max()
+    assert torch.all((lse.cpu().double() - math.log(L)).abs() <= 4 * L * R.F32 + 2.0 ** -20)
