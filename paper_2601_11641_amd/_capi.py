@@ -438,7 +438,8 @@ def mod_cache_attn_fwd(shape: mod_cache_shape, cache: mod_cache, q, max_len: int
             if st == _stream(None):
                 workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
             else:   # of the stream that uses it: nothing else does before or after in another order
-                with torch.cuda.stream(torch.cuda.ExternalStream(st)):
+                # (address 0, the default stream, would make an ExternalStream some other one)
+                with torch.cuda.stream(torch.cuda.ExternalStream(st) if st else torch.cuda.default_stream()):
                     workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=q.device)
     elif hasattr(workspace, "nbytes") and workspace.nbytes < ws_bytes:
         raise ValueError(f"workspace has {workspace.nbytes} bytes, ws_bytes says {ws_bytes}")

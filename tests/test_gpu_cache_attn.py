@@ -604,3 +604,30 @@ def test_codes_stay_exact_under_any_scale(M, case, sv):
     off = (o.cpu().double() - want).abs()
     assert torch.all(off <= bound), (off / bound).max()
     assert torch.all((lse.cpu().double() - math.log(L)).abs() <= 4 * L * R.F32 + 2.0 ** -20)
+
+
+@pytest.mark.parametrize("how", ["current", "side", "side address", "default", "default address"])
+def test_workspace_belongs_to_the_stream_that_uses_it(M, monkeypatch, how):
+    """While another stream is the current one, also for the default stream,
+    whose address is 0."""
+    f = Filled(M, 2, 2, 5000, 128, 128, R.INT8, [5000, 5000], seed=4)
+    q = queries(2, 2, 1, 128, 2)
+    o0, _ = f.run(q, 5000)
+    qd, o = q.cuda(), torch.empty_like(q, device="cuda")
+    assert M.mod_cache_attn_workspace_bytes(f.shape, 2, 1, 5000) > 0
+    side, current = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    want, stream = {"current": (current.cuda_stream, None), "side": (side.cuda_stream, side),
+                    "side address": (side.cuda_stream, side.cuda_stream), "default": (0, torch.cuda.default_stream()),
+                    "default address": (0, 0)}[how]
+    seen, empty = [], torch.empty
+    def spy(*args, **kw):
+        seen.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*args, **kw)
+    with torch.cuda.stream(current):
+        monkeypatch.setattr(torch, "empty", spy)
+        M.mod_cache_attn_fwd(f.shape, f.ref, qd, 5000, None, None, None, 0.0, o, None, stream=stream)
+        monkeypatch.undo()
+    torch.cuda.synchronize()
+    assert seen == [want]
+    assert torch.equal(o, o0)
