@@ -177,3 +177,73 @@ def test_struct_layouts_match_the_header(M, tmp_path):
         cls = getattr(M, t)
         want += [ctypes.sizeof(cls)] + [getattr(cls, f).offset for f in fs]
     assert got == want
+
+
+@pytest.fixture
+def anywhere(M, monkeypatch):
+    """Tensors of the host stand for tensors of the current device."""
+    monkeypatch.setattr(M._capi, "_device", lambda x, what: None)
+    monkeypatch.setattr(M._capi, "_current_device", lambda: -1)
+    return monkeypatch
+
+
+def calls(M, s, c):
+    """Calls with that cache that get past the binding's checks and no further:
+    a length, then a query head count that the library refuses."""
+    return [lambda: M.mod_cache_write(s, c, A, A, 0, None, None, 0, 0), lambda: M.mod_cache_read(s, c, A, A, 0, None, None, 0, 0),
+            lambda: M.mod_cache_attn_fwd(s, c, A, 1, None, None, None, 0.0, A, None, None, 0, 0, 0, 1)]
+
+
+@pytest.mark.parametrize("shape", [
+    (1, 2, 201, 64, 64), (1, 2, 200, 128, 64), (1, 2, 200, 64, 128), (2, 2, 200, 64, 64), (1, 3, 200, 64, 64),
+    (1, 2, 1 << 24, 64, 64), (1, 2, 199, 64, 64), (2, 1, 200, 64, 64), (1, 2, 100, 128, 64),
+])
+def test_cache_of_another_shape_refused(M, anywhere, shape):
+    """The tensors that a cache was made of are those of the call's shape: larger
+    ones would be read and written past their end, others in the wrong places."""
+    torch = pytest.importorskip("torch")
+    codes = lambda *n: torch.zeros(n, dtype=torch.uint8)   # noqa: E731
+    c = M.make_cache(codes(1, 2, 200, 64), codes(1, 2, 200, 64), torch.zeros(1, 2, 4), torch.zeros(1, 2, 4))
+    for call in calls(M, M.make_cache_shape(1, 2, 200, 64, 64), c):
+        assert refused(M, call) == 1
+    for call in calls(M, M.make_cache_shape(*shape), c):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_cache_of_one_dimension_and_of_addresses(M, anywhere):
+    torch = pytest.importorskip("torch")
+    s, f32 = M.make_cache_shape(1, 2, 200, 64, 64), torch.float32
+    flat = lambda n, t: torch.zeros(n, dtype=t)            # noqa: E731
+    for kn, vn, ksn, vsn, fits in ((25600, 25600, 8, 8, True), (30000, 25600, 9, 8, True), (25599, 25600, 8, 8, False),
+                                   (25600, 25599, 8, 8, False), (25600, 25600, 7, 8, False), (25600, 25600, 8, 7, False)):
+        c = M.make_cache(flat(kn, torch.uint8), flat(vn, torch.uint8), flat(ksn, f32), flat(vsn, f32))
+        for call in calls(M, s, c):
+            if fits:
+                assert refused(M, call) == 1
+            else:
+                with pytest.raises(ValueError):
+                    call()
+    # addresses are taken as they are, also where one is put into the struct later
+    for call in calls(M, s, M.make_cache(A, A, A, A)):
+        assert refused(M, call) == 1
+    c = M.make_cache(flat(25599, torch.uint8), flat(25600, torch.uint8), flat(8, f32), flat(8, f32))
+    c.k = A
+    for call in calls(M, s, c):
+        assert refused(M, call) == 1
+
+
+def test_cache_of_another_device_refused(M, anywhere):
+    torch = pytest.importorskip("torch")
+    codes = torch.zeros(1, 2, 200, 64, dtype=torch.uint8)
+    c = M.make_cache(codes, codes.clone(), torch.zeros(1, 2, 4), torch.zeros(1, 2, 4))
+    anywhere.setattr(M._capi, "_current_device", lambda: 1)
+    for call in calls(M, M.make_cache_shape(1, 2, 200, 64, 64), c):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_shapes_without_a_block_refused(M):
+    s, c = M.make_cache_shape(1, 2, 200, 64, 0), M.mod_cache(A, A, A, A)
+    for call in calls(M, s, c):
+        assert refused(M, call) == 2
