@@ -315,7 +315,8 @@ typedef struct mod_rope mod_rope;   /* opaque, library-owned */
  * that device may share it. */
 mod_status mod_rope_create(const mod_rope_params* params, mod_rope** out);
 
-/* Release the handle (waits for the device).  NULL is accepted. */
+/* Release the handle (waits for its device, whichever is the current one).
+ * NULL is accepted. */
 mod_status mod_rope_destroy(mod_rope* rope);
 
 /* y = R x in fp32, rounded to bf16 once.  B, H, L, d, text_tokens of the shape

@@ -233,8 +233,12 @@ mod_status mod_rope_create(const mod_rope_params* params, mod_rope** out) {
 
 mod_status mod_rope_destroy(mod_rope* rope) {
     if (!rope) return MOD_OK;
+    int device = rope->device;                       // the current one, where it is another
+    (void)hipGetDevice(&device);
+    if (device != rope->device) (void)hipSetDevice(rope->device);
     const hipError_t e = hipDeviceSynchronize();
     (void)hipFree(rope->table);
+    if (device != rope->device) (void)hipSetDevice(device);
     delete rope;
     if (e != hipSuccess) return hip_fail(e, "synchronise before destroy");
     return MOD_OK;
