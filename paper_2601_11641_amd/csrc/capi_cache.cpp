@@ -212,6 +212,7 @@ mod_status mod_rope_create(const mod_rope_params* params, mod_rope** out) {
     }
     hipError_t e = hipMalloc(reinterpret_cast<void**>(&r->table), table.size() * sizeof(float2));
     if (e != hipSuccess) {
+        (void)hipGetLastError();        // kept for the next launch's check otherwise
         delete r;
         return fail(MOD_ERR_NOMEM, "hipMalloc(%zu): %s", table.size() * sizeof(float2), hipGetErrorString(e));
     }

@@ -91,3 +91,14 @@ def test_destroy_waits_for_the_handles_device(tmp_path):
     std::printf("now on %d\n", device);
     """)
     assert out == ["wait for 1", "destroy", "wait for 1", "free on 1", "now on 0"]
+
+
+def test_a_failed_allocation_does_not_fail_the_next_call(tmp_path):
+    """The runtime keeps an error until it is asked for; a launch asks."""
+    out = run(tmp_path, r"""
+    if (mod_rope_create(&p, &a)) return 1;
+    room = 0;
+    if (mod_rope_create(&p, &b) != MOD_ERR_NOMEM || b) return 1;
+    std::printf("then %d\n", (int)mod_rope_fwd(a, &shape, x, nullptr, y, nullptr, 0, nullptr, nullptr));
+    """)
+    assert out[-1] == "then 0"
