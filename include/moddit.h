@@ -423,6 +423,12 @@ mod_status mod_cache_attn_fwd(const mod_cache_shape* shape, const mod_cache* cac
 
 /* ---- introspection (synchronous copies to host memory; for tests) ---- */
 
+/* How mod_cache_attn_fwd cuts up a call of these sizes, without lists or with
+ * them: the rows of a tile (16, 32, 64, 128 or 256) and the parts of a walk over
+ * the cache (1: whole).  Host only. */
+mod_status mod_cache_attn_plan(const mod_cache_shape* shape, int Hq, int Lq, int max_len, int lists, int* rows,
+                               int* parts);
+
 /* The sizes below count the nv video blocks (nv = n without text tokens). */
 
 /* Anchor `slot` (0 = newest, 1 = the one before): coefficients

@@ -116,6 +116,8 @@ _SIGS = {
     "mod_cache_read": (c_int, [POINTER(mod_cache_shape), POINTER(mod_cache), c_void_p, POINTER(mod_strides),
                                c_void_p, POINTER(mod_strides), c_int, c_int, c_void_p, c_void_p, c_void_p]),
     "mod_cache_attn_workspace_bytes": (c_size_t, [POINTER(mod_cache_shape), c_int, c_int, c_int]),
+    "mod_cache_attn_plan": (c_int, [POINTER(mod_cache_shape), c_int, c_int, c_int, c_int, POINTER(c_int),
+                                    POINTER(c_int)]),
     "mod_cache_attn_fwd": (c_int, [POINTER(mod_cache_shape), POINTER(mod_cache), c_void_p, c_int, c_int, c_int,
                                    c_void_p, c_void_p, c_void_p, c_float, c_void_p, c_void_p, c_void_p, c_size_t,
                                    c_void_p]),
@@ -456,6 +458,14 @@ def mod_cache_read(shape: mod_cache_shape, cache: mod_cache, k, v, first: int = 
 
 def mod_cache_attn_workspace_bytes(shape: mod_cache_shape, Hq: int, Lq: int, max_len: int) -> int:
     return int(_lib.mod_cache_attn_workspace_bytes(_ref(shape), Hq, Lq, max_len))
+
+
+def mod_cache_attn_plan(shape: mod_cache_shape, Hq: int, Lq: int, max_len: int, lists: bool = False):
+    """(rows of a tile, parts of a walk) of such a call."""
+    rows, parts = c_int(), c_int()
+    _check(_lib.mod_cache_attn_plan(_ref(shape), Hq, Lq, max_len, int(bool(lists)), ctypes.byref(rows),
+                                    ctypes.byref(parts)), "mod_cache_attn_plan")
+    return rows.value, parts.value
 
 
 def mod_cache_attn_fwd(shape: mod_cache_shape, cache: mod_cache, q, max_len: int, kv_len, kv_idx, kv_cnt,

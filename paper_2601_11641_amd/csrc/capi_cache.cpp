@@ -306,6 +306,18 @@ size_t mod_cache_attn_workspace_bytes(const mod_cache_shape* shape, int Hq, int 
     return plan_attn(shape, Hq, Lq, max_len, plans);
 }
 
+mod_status mod_cache_attn_plan(const mod_cache_shape* shape, int Hq, int Lq, int max_len, int lists, int* rows,
+                               int* parts) {
+    const mod_status st = check_attn(shape, Hq, Lq, max_len);
+    if (st != MOD_OK) return st;
+    if (!rows || !parts) return fail(MOD_ERR_INVALID_ARG, "rows and parts must not be NULL");
+    moddit::CacheAttnPlan plans[2];
+    plan_attn(shape, Hq, Lq, max_len, plans);
+    *rows = plans[lists != 0].rows;
+    *parts = plans[lists != 0].C;
+    return MOD_OK;
+}
+
 mod_status mod_cache_attn_fwd(const mod_cache_shape* shape, const mod_cache* cache, const void* q, int Hq, int Lq,
                               int max_len, const int32_t* kv_len, const int32_t* kv_idx, const int32_t* kv_cnt,
                               float scale, void* o, float* lse, void* workspace, size_t ws_bytes, void* stream) {
