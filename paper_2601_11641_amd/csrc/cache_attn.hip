@@ -1046,15 +1046,17 @@ CacheAttnPlan plan_cache_attn(int B, int H, int d, int block, int Hq, int Lq, in
     const int rows = lists ? std::min(block, Lq) : (int)std::min<long>((long)(Hq / H) * Lq, 1L << 30);
     CacheAttnPlan best{};
     double least = 0.0;
+    // bytes of the call's codes, q and o (small calls: 64 MB, no matter to anyone)
+    const double room = std::max(64e6, (2.0 * H * max_len + 4.0 * Hq * Lq) * B * d);
     // Work-groups run in rounds; the rows of a tile and the parts of a walk are
     // chosen so that the rounds end first by this estimate.  The lengths of lists
     // are not known here: they are taken to keep a quarter.  What the choice does:
-    // one query over 24 heads of 118,800 tokens 648 us whole, 207 in 4 parts, 132
-    // in 10 (240 work-groups, taken), 148 in 16; 8 heads of 8192 46 us whole, 9.7 in
-    // 32 parts (taken).  1024 queries over 8 heads of 1024: 18 us in tiles of 32
-    // (taken), 23 in tiles of 128 and three parts.  One frame of 3600 queries over
-    // 24 heads' lists is 696 tiles of 128, two rounds, the second short: 1.50 ms
-    // whole, 1.42 in two parts, 1.40 in five (taken).
+    // one query over 24 heads of 118,800 tokens 801 us whole, 227 in 4 parts, 139
+    // in 10 (240 work-groups, taken), 160 in 16; 8 heads of 8192 54 us whole, 10.0 in
+    // 32 parts (taken).  1024 queries over 8 heads of 1024: 17.6 us in tiles of 32
+    // (taken), 22.9 in tiles of 128 and three parts.  One frame of 3600 queries over
+    // 24 heads' lists is 696 tiles of 128, two rounds, the second short: 1.64 ms
+    // whole, 1.52 in two parts, 1.51 in five (taken).
     for (const TileCost& t : kTileCosts) {
         // a tile more than half empty is never better; d = 64: three work-groups of
         // 128 rows share a compute unit and one of 256 leaves a third of it empty
@@ -1081,8 +1083,13 @@ CacheAttnPlan plan_cache_attn(int B, int H, int d, int block, int Hq, int Lq, in
             const double rounds = (double)((share + slots / kXcds - 1) / (slots / kXcds));
             const double us = (t.turn + t.more * (double)std::min<long>(items, slots) / 256) * (d == 64 ? t.half : 1.0);
             const double join = c == 1 ? 0.0 : 5.0 + 0.02 * c + 1.3e-6 * items * std::min(t.rows, rows) * d;
-            // (parts, and the memory they take, have to save 1%)
-            const double cost = (rounds * (walk / c * us + t.start) + join) * (c == 1 ? 1.0 : 1.01);
+            // Parts have to save 1%, and 1% more for every quarter of the call's bytes
+            // that they take as workspace past the first: each graph or stream keeps
+            // one.  10,800 queries, 24 heads of 118,800 tokens (863 MB): four parts, 545
+            // MB, 15.8 ms; six took 818 MB and 15.7 ms, whole tiles 18.2.
+            const double held = (double)items * t.rows * (d + 1) * 4 / room;
+            const double extra = c == 1 ? 0.0 : 0.01 + std::max(0.0, 0.04 * (held - 0.25));
+            const double cost = (rounds * (walk / c * us + t.start) + join) * (1.0 + extra);
             if (least == 0.0 || cost < least) {
                 least = cost;
                 best = p;

@@ -54,3 +54,32 @@ def test_plan_refusals(M):
         assert lib.mod_cache_attn_plan(ctypes.byref(s), 2, 1, 100, 0, rows and ctypes.byref(rows),
                                        parts and ctypes.byref(parts)) == 1
     assert M.mod_cache_attn_plan(s, 2, 1, 0) == (16, 1)
+
+
+def call_bytes(B, H, Hq, Lq, L, d):
+    """Codes of the call's tokens, q and o; 64 MB at least."""
+    return max(64e6, B * d * (2 * H * L + 4 * Hq * Lq))
+
+
+@pytest.mark.parametrize("B,H,Hq,Lq,L,d,most", [
+    (1, 24, 24, 10800, 118800, 128, 600e6),      # a chunk of three frames: under its cache's 730 MB
+    (1, 24, 24, 10800, 118800, 64, 300e6),
+    (1, 24, 24, 3600, 118800, 128, 340e6),
+    (7, 2, 16, 7447, 127292, 128, 1300e6),
+    (7, 2, 16, 3000, 60000, 128, 600e6),
+])
+def test_workspace_of_many_rows_is_worth_it(M, B, H, Hq, Lq, L, d, most):
+    s = M.make_cache_shape(B, H, L, d, 128, "int8")
+    assert M.mod_cache_attn_workspace_bytes(s, Hq, Lq, L) <= most
+
+
+def test_workspace_is_bounded(M):
+    """By four times the bytes of the call's own tensors, and 2.2 GB."""
+    for B in (1, 3, 16):
+        for H, Hq in ((1, 1), (1, 16), (5, 40), (24, 24), (46, 92)):
+            for Lq in (1, 17, 300, 2444, 9621):
+                for L in (100, 9241, 34672, 90719, 250000):
+                    for d, block in ((64, 64), (128, 128)):
+                        s = M.make_cache_shape(B, H, L, d, block, "int8")
+                        need = M.mod_cache_attn_workspace_bytes(s, Hq, Lq, L)
+                        assert need <= min(2.2e9, 4 * call_bytes(B, H, Hq, Lq, L, d)), (B, H, Hq, Lq, L, d)
