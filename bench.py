@@ -607,7 +607,7 @@ def run_stream(args):
         cs = M.make_cache_shape(cfg.B, cfg.H, cfg.L, cfg.d, cfg.block, fmt)
         cache = M.Cache(cs, dev)
         whole_write_ms = timed(lambda: M.mod_cache_write(cs, cache.ref, k, v))
-        cws = torch.empty(max(M.mod_cache_attn_workspace_bytes(cs, cfg.H, n_q, cfg.L) for n_q in (L, cfg.L)) or 1,
+        cws = torch.empty(max(M.mod_cache_attn_workspace_bytes(cs, cfg.H, n_q, cfg.L) for n_q in (1, L, cfg.L)) or 1,
                           dtype=torch.uint8, device=dev)
         sparse = lambda: M.mod_cache_attn_fwd(cs, cache.ref, q, cfg.L, None, kv_idx, kv_cnt, 0.0, out, lse,  # noqa: E731
                                               cws, cws.numel())
