@@ -268,8 +268,8 @@ mod_status mod_block_sparse_attn_fwd_noalloc(const mod_shape* shape, const void*
  * frames made so far.  Per layer and chunk: rotate the new queries and keys
  * (mod_rope_fwd), write the new keys and values into the cache
  * (mod_cache_write) and attend from the new queries to what the cache holds
- * (mod_cache_attn_fwd), over every block or over lists of kept blocks such as
- * mod_predict_block_mask selects.  Single tokens are served by the same calls.
+ * (mod_cache_attn_fwd), over every block or over lists of kept blocks.  Single
+ * tokens are served by the same calls.
  *
  * The operands may sit as the projection left them: a tensor argument with a
  * mod_strides is [B, H, L, d] with d contiguous and the other axes that many
@@ -410,13 +410,22 @@ size_t mod_cache_attn_workspace_bytes(const mod_cache_shape* shape, int Hq, int 
  * / block) blocks for every block of `block` query tokens (nq = ceil(Lq /
  * block)): kv_idx [B, Hq, nq, n], kv_cnt [B, Hq, nq] (clamped to [0, n]), the
  * layout of mod_predict_block_mask; entries outside [0, n) and blocks past the
- * sequence's end are skipped, each block is listed at most once.
+ * sequence's end are skipped, each block is listed at most once.  Row i of the
+ * lists is for query tokens i * block .. of this call.  mod_predict_block_mask
+ * counts query blocks from the sequence's first token and takes q and k of the
+ * whole sequence, so its rows are a call's own where the call's queries start at
+ * the start of a block of the sequence (rows first / block on).
  * A row that keeps no token gives O = 0 and lse = -inf.  scale = 0 means
  * 1/sqrt(d).  q, k and v enter bf16 MFMA products without error (every code is
- * a bf16 number); probabilities, times the value scale, are rounded to bf16 (to
- * two bf16, about 2^-17, where a head's rows are at most 16); sums, softmax and
- * accumulation are fp32.  The result does not depend on
- * anything outside the sequence's own tokens, and is the same in every run. */
+ * a bf16 number); probabilities, times the value scale, are rounded to bf16, or to
+ * two bf16 (at most 2^-16 off) where the call takes tiles of 16 rows: always
+ * where at most 16 rows share a walk (Hq / H * Lq; with lists min(block, Lq)), and
+ * for some calls with more.  Sums, softmax and accumulation are fp32 (a sum of
+ * probabilities times values has to stay below its 3.4e38).
+ * No value outside the sequence's own tokens enters the result, and calls of the
+ * same sizes give the same bits in every run.  Calls of other B, H, Hq, Lq or
+ * max_len may sum the same tokens in other groups, and round their
+ * probabilities once or twice as above. */
 mod_status mod_cache_attn_fwd(const mod_cache_shape* shape, const mod_cache* cache, const void* q, int Hq, int Lq,
                               int max_len, const int32_t* kv_len, const int32_t* kv_idx, const int32_t* kv_cnt,
                               float scale, void* o, float* lse, void* workspace, size_t ws_bytes, void* stream);
