@@ -13,7 +13,8 @@
 // join_kernel joins the parts of a walk:
 //   rows_kernel   16 or 32 rows: few rows, bound by reading the cache, or calls
 //                 too small to fill the chip, bound by the turns of a walk;
-//   tile_kernel   64, 128 or 256 rows: bound by the matrix cores' power.
+//   tile_kernel   64, 128 or 256 rows: bound by the card's power, which the
+//                 conversions of the codes share with the matrix products.
 // Without lists the query heads of a key/value head share a tile (their rows
 // are consecutive in memory).
 //
@@ -28,9 +29,13 @@
 //       belong to are those whose V it loads (D/16 consecutive channels
 //       each), so P needs no exchange between lanes and V^T is formed by
 //       byte permutes of the lane's own loads.
-// One query over 24 heads of 118,800 tokens of 128 channels (730 MB) takes 132
-// us: 5.5 TB/s, where a large copy moves 4.9.  With one step's codes and no
-// more under way it took 177 us.
+// One query over 24 heads of 118,800 tokens of 128 channels (730 MB) takes 131
+// us: 5.6 TB/s, where a large copy moves 4.9; over lists of a quarter of the
+// blocks 35 us (5.2).  With one step's codes and no more under way the first took
+// 177 us.
+// A wave that meets a value scale under 2^-64 walks its steps twice (see
+// small_scale): products apart from the accumulators in the one loop cost 6% of a
+// call with 16 rows and 19% of one with 32.
 #include "moddit_internal.h"
 
 #include <algorithm>
@@ -462,13 +467,17 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void rows_kernel(AttnArgs a) {
 // With 256 rows one work-group fills a compute unit, with fewer two share it
 // (three at d = 64).
 //
-// 10,800 queries over 24 heads of 118,800 tokens (15.8 TFLOP): int8 15.0 ms,
-// 1.05 PFLOP/s (e4m3 1.09), where a bf16 matrix product of 8192 reaches 1.28.
-// The clock falls as the matrix cores are kept busier (half of the cycles at 2.0
-// GHz), so what is left is energy, not stalls: three buffers with the barrier
-// off the critical path saved 6% of the cycles and no time, reads further
-// ahead, priorities, other orders of a half and a layout without the staging
-// writes' bank conflicts (a sixth of the LDS cycles) nothing.  Phases of scores
+// 10,800 queries over 24 heads of 118,800 tokens (15.8 TFLOP): int8 15.5 ms,
+// 1.02 PFLOP/s (e4m3 14.6, 1.08), where a bf16 matrix product of 16384 reaches
+// 1.38.  The matrix cores are busy in half of the cycles at 2.0 GHz, beside 7.7
+// vector instructions to a matrix instruction: every tile converts the codes it
+// reads again, through registers and LDS writes.  (This library's attention over
+// bf16, which copies tiles into LDS as they are, has 4.1, 0.73 and 1.53 GHz.)
+// Changes that leave the conversions cost what they saved at a lower clock:
+// three buffers with the barrier off the critical path saved 6% of the cycles and
+// no time, reads further ahead, priorities, other orders of a half and a layout
+// without the staging writes' bank conflicts (a sixth of the LDS cycles)
+// nothing.  Phases of scores
 // and softmax behind barriers took 17.1 ms, rows_kernel alone 28.6; unrolling
 // the loop by buffer spilled and took 35.
 // 8-bit products of the codes of K with q as two E4M3 parts (exact down to 2^-21
@@ -1029,7 +1038,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttnArgs a) {
 // each work-group per compute unit adds to it, its start and end, and how much of
 // a turn d = 64 takes.  A fit to 11,000 calls with 1 to 16,384 queries, 64 to
 // 185,000 tokens, with and without lists, each with up to 60 ways to cut it up:
-// the way chosen by it is 2% slower than the best one measured, on average.
+// the way chosen by it was 2% slower than the best one measured, on average,
+// before workspace had a price.
 struct TileCost {
     int rows;
     double turn, more, start, half;
