@@ -352,9 +352,9 @@ def make_cache_shape(B, H, capacity, d, block, format="e4m3") -> mod_cache_shape
 
 def make_cache(k, v, k_scale, v_scale) -> mod_cache:
     """The cache in these tensors (codes [B, H, capacity, d] of one byte, fp32
-    scales [B, H, n], or one-dimensional ones that hold as many), which the
-    caller keeps alive: the struct holds their addresses.  The calls refuse a
-    cache shape that its tensors do not have."""
+    scales [B, H, n]; with other numbers of axes as many elements, with one axis
+    at least as many), which the caller keeps alive: the struct holds their
+    addresses.  The calls refuse a cache shape that its tensors do not have."""
     for x, what in ((k, "k"), (v, "v")):
         if hasattr(x, "element_size") and x.element_size() != 1:
             raise ValueError(f"{what} must have one byte per code, got {x.dtype}")
@@ -385,7 +385,8 @@ def _check_cache(shape, cache):
     for name, got, address, want in zip(("k", "v", "k_scale", "v_scale"), shapes, at, (codes, codes, scales, scales)):
         if got is None or got == want or getattr(cache, name) != address:
             continue
-        if len(got) != 1 or got[0] < math.prod(want):
+        held, needed = math.prod(got), math.prod(want)
+        if len(got) == len(want) or held < needed or (held > needed and len(got) > 1):
             raise ValueError(f"the cache's {name} has shape {got}, the cache shape says {want}")
     cache.fits = bytes(shape)
 

@@ -247,3 +247,19 @@ def test_shapes_without_a_block_refused(M):
     s, c = M.make_cache_shape(1, 2, 200, 64, 0), M.mod_cache(A, A, A, A)
     for call in calls(M, s, c):
         assert refused(M, call) == 2
+
+
+def test_cache_of_merged_axes(M, anywhere):
+    """[B * H, capacity, d] and [B * H, n] hold the same in the same order."""
+    torch = pytest.importorskip("torch")
+    s = M.make_cache_shape(2, 3, 200, 64, 64)
+    for codes, scales, fits in (((6, 200, 64), (6, 4), True), ((1200, 64), (24,), True), ((6, 201, 64), (6, 4), False),
+                                ((6, 199, 64), (6, 4), False), ((6, 200, 64), (6, 5), False), ((6, 200, 64), (6, 3), False),
+                                ((3, 2, 200, 64), (6, 4), False), ((6, 200, 64), (3, 2, 4), False)):
+        c = M.make_cache(*(torch.zeros(codes, dtype=torch.uint8) for _ in range(2)), *(torch.zeros(scales) for _ in range(2)))
+        for call in calls(M, s, c):
+            if fits:
+                assert refused(M, call) == 1
+            else:
+                with pytest.raises(ValueError):
+                    call()
