@@ -1056,8 +1056,8 @@ CacheAttnPlan plan_cache_attn(int B, int H, int d, int block, int Hq, int Lq, in
     const int rows = lists ? std::min(block, Lq) : (int)std::min<long>((long)(Hq / H) * Lq, 1L << 30);
     CacheAttnPlan best{};
     double least = 0.0;
-    // bytes of the call's codes, q and o (small calls: 64 MB, no matter to anyone)
-    const double room = std::max(64e6, (2.0 * H * max_len + 4.0 * Hq * Lq) * B * d);
+    // bytes of the call's codes, q and o (small calls: 256 MB, a thousandth of the memory)
+    const double room = std::max(256e6, (2.0 * H * max_len + 4.0 * Hq * Lq) * B * d);
     // Work-groups run in rounds; the rows of a tile and the parts of a walk are
     // chosen so that the rounds end first by this estimate.  The lengths of lists
     // are not known here: they are taken to keep a quarter.  What the choice does:
