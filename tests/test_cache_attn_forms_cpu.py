@@ -74,7 +74,7 @@ def test_workspace_of_many_rows_is_worth_it(M, B, H, Hq, Lq, L, d, most):
 
 
 def test_workspace_is_bounded(M):
-    """By twice the bytes of the call's own tensors, and 2.2 GB."""
+    """By three times the bytes of the call's own tensors, and 2.2 GB."""
     for B in (1, 3, 16):
         for H, Hq in ((1, 1), (1, 16), (5, 40), (24, 24), (46, 92)):
             for Lq in (1, 17, 300, 2444, 9621):
@@ -82,4 +82,4 @@ def test_workspace_is_bounded(M):
                     for d, block in ((64, 64), (128, 128)):
                         s = M.make_cache_shape(B, H, L, d, block, "int8")
                         need = M.mod_cache_attn_workspace_bytes(s, Hq, Lq, L)
-                        assert need <= min(2.2e9, 2 * call_bytes(B, H, Hq, Lq, L, d)), (B, H, Hq, Lq, L, d)
+                        assert need <= min(2.2e9, 3 * call_bytes(B, H, Hq, Lq, L, d)), (B, H, Hq, Lq, L, d)
