@@ -420,8 +420,8 @@ size_t mod_cache_attn_workspace_bytes(const mod_cache_shape* shape, int Hq, int 
  * a bf16 number); probabilities, times the value scale, are rounded to bf16, or to
  * two bf16 (at most 2^-16 off) where the call takes tiles of 16 rows: always
  * where at most 16 rows share a walk (Hq / H * Lq; with lists min(block, Lq)), and
- * for some calls with more.  Sums, softmax and accumulation are fp32 (a sum of
- * probabilities times values has to stay below its 3.4e38).
+ * for some calls with more.  Sums, softmax and accumulation are fp32 (values up
+ * to 2^119 / max_len never overflow it).
  * No value outside the sequence's own tokens enters the result, and calls of the
  * same sizes give the same bits in every run.  Calls of other B, H, Hq, Lq or
  * max_len may sum the same tokens in other groups, and round their
